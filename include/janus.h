@@ -52,6 +52,11 @@ extern "C" {
                                        and janus_indexer_scores_batch, on tensor-core shapes only (else JANUS_ERR_UNSUPPORTED);
                                        janus_indexer_topk then works through a score matrix in its workspace */
 
+/* element types of janus_rope */
+#define JANUS_ELEM_BF16 0
+#define JANUS_ELEM_FP16 1
+#define JANUS_ELEM_FP32 2
+
 /* Library version (major*10000 + minor*100 + patch). */
 int janus_version(void);
 
@@ -339,6 +344,117 @@ int janus_sparse_attn_decode(const void* q, int B, int H_q, int d_qk,
                              const int32_t* page_tables, const int64_t* table_offsets,
                              float softmax_scale, void* out, float* lse,
                              int32_t* dev_status, void* stream);
+
+/*
+ * A step's plan, and the cache around the attention.  The paper has no counterpart; a serving loop makes these calls before (plan, rotary
+ * positions, rows into the cache) and beside (dense layers between the sparse ones) the calls above, with the same page tables.
+ *
+ * janus_batch_plan - page tables, rows, positions and cache places of a step, from the lengths of its sessions.  With c = cached_lens[b]
+ * (tokens in the cache), n = new_lens[b] (tokens of this step), t = c + n, p = page_size:
+ *
+ *   block_tables   [B, width] int32, row stride block_ld; in: row b holds the pages of session b's cached tokens, ceil(c / p) of
+ *                  them; out: the ceil(t / p) - ceil(c / p) further ones are written behind them, taken from
+ *   free_pages     [n_free] int32 from its beginning on, sessions in order (an id is taken once; the caller removes counts[0] of them)
+ *   row_offsets    [B + 1] int64 out: new tokens of session b are rows row_offsets[b] .. row_offsets[b + 1] of the step
+ *   kv_lens        [B] int64 out: t
+ *   table_offsets  [B + 1] int64 out, page_tables [table_capacity] int32 out: the sessions' page tables one behind the other, as
+ *                  janus_page_demand_batch, janus_sparse_attn_decode and janus_attn_decode_shared take them; entries behind the last
+ *                  table are left as they were
+ *   row_sessions, positions, slots   [max_rows] int32, int64, int64 out: session of a row, position c + i of its token, and its
+ *                  place in the pool, page * p + position % p; rows behind the last one are written -1
+ *   key_rows       [max_rows] int64 out, or NULL: key_offsets[b] + position, the row of the token's indexer key where session b's keys begin
+ *                  at row key_offsets[b] (given with it; -1 where slots is -1)
+ *   counts         [3] int64 out: pages taken, table entries, rows; the true numbers where a capacity was exceeded
+ *
+ * cached_lens is what janus_page_demand_batch takes as demand_limits.  An entry of length 0 stands empty.  Where lists are too short (free
+ * pages, page_tables, rows, or a session longer than width * p) the call reports JANUS_DEV_CAPACITY_EXCEEDED: a page that could not be
+ * taken, and the slot of a token without a page, is -1, offsets and lengths are cut back to what is there.  A negative length counts as 0, and a
+ * page id outside [0, n_phys_pages) as -1, with JANUS_DEV_INDEX_OUT_OF_RANGE.  B <= 8192 and B * width < 2^31, else JANUS_ERR_UNSUPPORTED.
+ */
+int janus_batch_plan(const int64_t* cached_lens, const int64_t* new_lens, int B, int page_size,
+                     int32_t* block_tables, int64_t block_ld, int64_t width,
+                     const int32_t* free_pages, int64_t n_free, int64_t n_phys_pages, const int64_t* key_offsets,
+                     int64_t* row_offsets, int64_t* kv_lens, int64_t* table_offsets,
+                     int32_t* page_tables, int64_t table_capacity,
+                     int32_t* row_sessions, int64_t* positions, int64_t* slots, int64_t* key_rows, int64_t max_rows,
+                     int64_t* counts, int32_t* dev_status, void* stream);
+
+/*
+ * janus_rope - rotary positions on dims [rot_offset, rot_offset + rot_dim) of every head: pair i is turned by positions[t] * f_i,
+ *
+ *     (y1, y2) = scale * (x1 cos a - x2 sin a, x1 sin a + x2 cos a)
+ *
+ * in fp32, rounded once.  Pairs are dims (2i, 2i + 1) of the rotated part when `interleaved`, else (i, i + rot_dim / 2).  `inverse`
+ * turns by -a: what takes the gradient of y to that of x.  The other dims are copied.
+ *
+ *   x, out      [T, H, D] bf16, fp16 or fp32 (JANUS_ELEM_*), any strides of rows and heads (in elements); out is x itself, with its
+ *               strides, or memory that shares nothing with it
+ *   positions   [T] int64; a negative one marks a padding row, whose part of `out` is left as it was
+ *   freqs       [rot_dim / 2] uint64: f_i / (2 pi), turns per position, in units of 2^-64.  The angle of a position below 2^31 is then exact to
+ *               2^-33 turns before it is rounded to fp32
+ *   scale       factor on the rotated dims (1, or what the stretching of the frequencies asks for)
+ */
+int janus_rope(const void* x, int64_t x_row_stride, int64_t x_head_stride, int64_t T, int H, int D,
+               const int64_t* positions, const uint64_t* freqs, int rot_offset, int rot_dim, int interleaved,
+               float scale, int inverse, int dtype,
+               void* out, int64_t out_row_stride, int64_t out_head_stride, void* stream);
+
+/*
+ * janus_rope_append - the new rows of a step into the paged cache: keys rotated as by janus_rope, values copied; queries, where
+ * given, rotated to q_out in the same launch.  All bf16.
+ *
+ *   q, q_out    [T, H_q, d_qk], both NULL or both given; q_out may be q (with its strides)
+ *   k           [T, n_kv_heads, d_qk] -> k_pool, v [T, n_kv_heads, d_v] -> v_pool; v and v_pool both NULL for the latent layout, whose
+ *               values are part of the key rows
+ *   positions   [T] int64; slots [T] int64: row t goes to token slots[t] % page_size of page slots[t] / page_size.  Rows of slot -1
+ *               are not written, queries of a negative position neither (padding).  A slot beyond the pool, or a slot with a negative
+ *               position, is skipped with JANUS_DEV_INDEX_OUT_OF_RANGE.  Slots of one call are distinct; of two rows for one slot it is not said
+ *               which bytes stay.
+ *   pools       strides in elements as for janus_sparse_attn_prefill, of k_pool and of v_pool each; bases and all strides on 16 bytes,
+ *               d_qk and d_v multiples of 8
+ */
+int janus_rope_append(const void* q, int64_t q_row_stride, int64_t q_head_stride, int H_q,
+                      const void* k, int64_t k_row_stride, int64_t k_head_stride, int n_kv_heads, int d_qk,
+                      const void* v, int64_t v_row_stride, int64_t v_head_stride, int d_v,
+                      int64_t T, const int64_t* positions, const int64_t* slots,
+                      const uint64_t* freqs, int rot_offset, int rot_dim, int interleaved, float scale,
+                      void* q_out, int64_t q_out_row_stride, int64_t q_out_head_stride,
+                      void* k_pool, int64_t k_page_stride, int64_t k_tok_stride, int64_t k_pool_head_stride,
+                      void* v_pool, int64_t v_page_stride, int64_t v_tok_stride, int64_t v_pool_head_stride,
+                      int page_size, int64_t n_phys_pages, int32_t* dev_status, void* stream);
+
+/*
+ * janus_attn_decode_shared - dense attention of one query token per session, for a batch whose sessions share their first prefix_len tokens
+ * (a common system prompt or document).  With P = prefix_len and t = kv_lens[b]:
+ *
+ *     out[b, h, :] = sum_{s < t} softmax_s( softmax_scale * < q[b, h, :], K_s > ) * V_s
+ *
+ * where token s < P lies in page prefix_table[s / page_size], and token s >= P in page page_tables[table_offsets[b] + s / page_size] (a
+ * session's table covers it from its first token on, as janus_batch_plan makes it; the entries of the shared tokens are not read).
+ * The rows of the prefix are read once for all sessions.
+ *
+ *   q          [B, H_q, d_qk] bf16, dense; out [B, H_q, d_v] bf16; lse [B, H_q] fp32 (log-sum-exp of the scaled logits) or NULL
+ *   pools      as for janus_sparse_attn_prefill, with strides of their own for v_pool; v_pool may be k_pool, with its strides; n_phys_pages
+ *              pages
+ *   kv_lens    [B] int64: 0 marks an entry that stands empty (zeros, lse -inf), every other length is at least P.  max_len, a host value,
+ *              bounds them (and is at least P)
+ *   ws         janus_attn_decode_shared_workspace_size(...) bytes, 16-byte aligned; contents undefined on return, calls that share it
+ *              must not overlap on the device
+ *
+ * A row none of whose logits is above -inf gives zeros.  Tokens whose page is missing or outside [0, n_phys_pages) are skipped, a length
+ * below P empties its entry and one above max_len is cut back, each with JANUS_DEV_INDEX_OUT_OF_RANGE.  softmax_scale > 0.  d_qk and d_v
+ * multiples of 8, d_qk <= 576, d_v <= 512, H_q a multiple of n_kv_heads; bases and strides on 16 bytes.
+ */
+size_t janus_attn_decode_shared_workspace_size(int B, int H_q, int d_qk, int n_kv_heads, int d_v, int page_size,
+                                               int64_t prefix_len, int64_t max_len);
+int janus_attn_decode_shared(const void* q, int B, int H_q, int d_qk,
+                             const void* k_pool, int64_t k_page_stride, int64_t k_tok_stride, int64_t k_head_stride,
+                             const void* v_pool, int64_t v_page_stride, int64_t v_tok_stride, int64_t v_head_stride,
+                             int n_kv_heads, int d_v, int page_size, int64_t n_phys_pages,
+                             const int32_t* prefix_table, int64_t prefix_len,
+                             const int32_t* page_tables, const int64_t* table_offsets, const int64_t* kv_lens, int64_t max_len,
+                             float softmax_scale, void* out, float* lse,
+                             void* ws, size_t ws_bytes, int32_t* dev_status, void* stream);
 
 /*
  * Diagnostics.  The paper has no counterpart for either call.

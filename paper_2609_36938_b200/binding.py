@@ -34,6 +34,7 @@ EXPORTS = [
     "janus_sparse_attn_prefill_workspace_size", "janus_sparse_attn_prefill",
     "janus_indexer_scores_batch", "janus_topk_batch", "janus_page_demand_batch", "janus_sparse_attn_decode",
     "janus_topk_entries", "janus_entry_expand", "janus_entry_pool_scores",
+    "janus_batch_plan", "janus_rope", "janus_rope_append", "janus_attn_decode_shared_workspace_size", "janus_attn_decode_shared",
     "janus_selftest_bounded_wait", "janus_fp8_mma_probe",
 ]
 
@@ -103,6 +104,19 @@ def load() -> ctypes.CDLL:
     lib.janus_entry_pool_scores.argtypes = [c_p, c_i64, c_i, c_i64, c_i64, c_i, c_i, c_p, c_i64, c_p]
     lib.janus_entry_expand.restype = c_i
     lib.janus_entry_expand.argtypes = [c_p, c_i, c_i, c_i, c_i64, c_p, c_p]
+    lib.janus_batch_plan.restype = c_i
+    lib.janus_batch_plan.argtypes = [c_p, c_p, c_i, c_i, c_p, c_i64, c_i64, c_p, c_i64, c_i64, c_p, c_p, c_p, c_p, c_p, c_i64, c_p, c_p, c_p, c_p, c_i64, c_p,
+                                     c_p, c_p]
+    lib.janus_rope.restype = c_i
+    lib.janus_rope.argtypes = [c_p, c_i64, c_i64, c_i64, c_i, c_i, c_p, c_p, c_i, c_i, c_i, c_f, c_i, c_i, c_p, c_i64, c_i64, c_p]
+    lib.janus_rope_append.restype = c_i
+    lib.janus_rope_append.argtypes = [c_p, c_i64, c_i64, c_i, c_p, c_i64, c_i64, c_i, c_i, c_p, c_i64, c_i64, c_i, c_i64, c_p, c_p, c_p, c_i, c_i, c_i, c_f,
+                                      c_p, c_i64, c_i64, c_p, c_i64, c_i64, c_i64, c_p, c_i64, c_i64, c_i64, c_i, c_i64, c_p, c_p]
+    lib.janus_attn_decode_shared_workspace_size.restype = c_sz
+    lib.janus_attn_decode_shared_workspace_size.argtypes = [c_i, c_i, c_i, c_i, c_i, c_i, c_i64, c_i64]
+    lib.janus_attn_decode_shared.restype = c_i
+    lib.janus_attn_decode_shared.argtypes = [c_p, c_i, c_i, c_i, c_p, c_i64, c_i64, c_i64, c_p, c_i64, c_i64, c_i64, c_i, c_i, c_i, c_i64, c_p, c_i64, c_p, c_p,
+                                             c_p, c_i64, c_f, c_p, c_p, c_p, c_sz, c_p, c_p]
     lib.janus_selftest_bounded_wait.restype = c_i
     lib.janus_selftest_bounded_wait.argtypes = [c_i, c_p, c_p, c_p]
     lib.janus_fp8_mma_probe.restype = c_i
@@ -330,6 +344,129 @@ def janus_sparse_attn_decode(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torc
     if table_offsets is None:
         raise JanusError("janus_sparse_attn_decode failed: JANUS_ERR_INVALID_ARG")
     return _native().sparse_attn(q, k_pool, v_pool, idx, page_tables, table_offsets, page_size, softmax_scale, d_v, want_lse, out)
+
+
+# ---- a step's plan, rotary positions and the cache, dense layers ----------------------------------------------------
+def batch_plan_buffers(B: int, max_rows: int, table_capacity: int, want_key_rows: bool = False, device="cuda") -> Dict[str, torch.Tensor]:
+    """Output buffers of janus_batch_plan.  Allocate once and pass as ``out=`` to keep allocations out of a serving loop."""
+    def empty(n, dtype):
+        return torch.empty((int(n),), dtype=dtype, device=device)
+
+    out = {"row_offsets": empty(B + 1, torch.int64), "kv_lens": empty(B, torch.int64), "table_offsets": empty(B + 1, torch.int64),
+           "page_tables": empty(table_capacity, torch.int32), "row_sessions": empty(max_rows, torch.int32), "positions": empty(max_rows, torch.int64),
+           "slots": empty(max_rows, torch.int64), "counts": empty(3, torch.int64)}      # counts: pages taken, table entries, rows
+    if want_key_rows:
+        out["key_rows"] = empty(max_rows, torch.int64)
+    return out
+
+
+def janus_batch_plan(cached_lens: torch.Tensor, new_lens: torch.Tensor, block_tables: torch.Tensor, free_pages: torch.Tensor, *, page_size: int,
+                     n_phys_pages: int, max_rows: int, key_offsets: Optional[torch.Tensor] = None, table_capacity: Optional[int] = None,
+                     out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+    """Page tables, rows, positions and cache places of a step from the lengths of its sessions (int64 [B] tensors on the device).
+    block_tables [B, width] int32 holds the pages of the cached tokens; the further pages come from the beginning of free_pages and are
+    written behind them.  key_offsets (int64 [B] or longer): also key_rows, the places of the indexer keys.  Returns a dict of device
+    tensors; the counts stay on the device (no host sync).  ``out``: buffers from batch_plan_buffers()."""
+    if out is None:
+        if table_capacity is None:
+            table_capacity = block_tables.shape[0] * block_tables.shape[1]
+        out = batch_plan_buffers(cached_lens.numel(), max_rows, table_capacity, key_offsets is not None, cached_lens.device)
+    return _native().batch_plan(cached_lens, new_lens, block_tables, free_pages, page_size, n_phys_pages, max_rows, key_offsets, out)
+
+
+def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: Optional[dict] = None, device="cuda") -> Tuple[torch.Tensor, float]:
+    """Frequency table of janus_rope / janus_rope_append, and the factor to pass as ``scale``.  Pair i turns by base^(-2i / rot_dim) radians
+    per position, scaled for long contexts by ``scaling``:
+
+      {"type": "linear", "factor"}      positions divided by the factor
+      {"type": "ntk", "factor"}         base multiplied by factor^(rot_dim / (rot_dim - 2)): the slowest pair is stretched by the factor, the fastest stays
+      {"type": "yarn", "factor", "original_max_position"[, "beta_fast" 32, "beta_slow" 1, "attention_factor"]}      pairs that turn more than beta_fast times over
+                                        the original context stay, those below beta_slow are stretched, a linear ramp between; the rotated values are
+                                        multiplied by attention_factor (0.1 ln(factor) + 1 unless given)
+      {"type": "wavelength", "factor", "low_freq_factor", "high_freq_factor", "original_max_position"}      the same two ends in terms of wavelength, with a ramp
+                                        that is linear in the frequency
+
+    The table holds turns per position in units of 2^-64 (int64, the bits of the library's uint64)."""
+    import math
+
+    rot_dim = int(rot_dim)
+    if rot_dim <= 0 or rot_dim % 2:
+        raise ValueError("rot_dim must be a positive even number")
+    if not (base > 0 and math.isfinite(base)):
+        raise ValueError("base must be a positive number")
+    scaling = dict(scaling or {"type": None})
+    kind, scale = scaling.pop("type"), 1.0
+    known = {None: set(), "linear": {"factor"}, "ntk": {"factor"},
+             "yarn": {"factor", "original_max_position", "beta_fast", "beta_slow", "attention_factor"},
+             "wavelength": {"factor", "low_freq_factor", "high_freq_factor", "original_max_position"}}
+    optional = {"beta_fast", "beta_slow", "attention_factor"}
+    if kind not in known:
+        raise ValueError(f"scaling type {kind!r}: one of linear, ntk, yarn, wavelength")
+    if set(scaling) - known[kind] or known[kind] - optional - set(scaling):
+        raise ValueError(f"scaling {kind!r} takes {sorted(known[kind])}")
+    factor = float(scaling.get("factor", 1.0))
+    if not (factor >= 1.0 and math.isfinite(factor)):
+        raise ValueError("factor must be at least 1")
+    if kind == "ntk" and rot_dim > 2:
+        base = base * factor ** (rot_dim / (rot_dim - 2))
+    f = [base ** (-2.0 * i / rot_dim) for i in range(rot_dim // 2)]
+    if kind == "linear":
+        f = [x / factor for x in f]
+    elif kind == "yarn":
+        old = float(scaling["original_max_position"])
+        if base <= 1:
+            raise ValueError("base must be above 1")
+
+        def pair_of(turns):      # the (fractional) pair that makes so many turns over the original context
+            return rot_dim * math.log(old / (turns * 2 * math.pi)) / (2 * math.log(base))
+
+        lo = max(math.floor(pair_of(float(scaling.get("beta_fast", 32.0)))), 0)
+        hi = min(math.ceil(pair_of(float(scaling.get("beta_slow", 1.0)))), rot_dim - 1)
+        ramp = [min(max((i - lo) / max(hi - lo, 0.001), 0.0), 1.0) for i in range(rot_dim // 2)]
+        f = [x / factor * r + x * (1.0 - r) for x, r in zip(f, ramp)]
+        scale = float(scaling.get("attention_factor", 0.1 * math.log(factor) + 1.0))
+    elif kind == "wavelength":
+        old, low, high = (float(scaling[k]) for k in ("original_max_position", "low_freq_factor", "high_freq_factor"))
+        if not high > low:
+            raise ValueError("high_freq_factor must be above low_freq_factor")
+        stay = [min(max((old * x / (2 * math.pi) - low) / (high - low), 0.0), 1.0) for x in f]
+        f = [x / factor * (1.0 - r) + x * r for x, r in zip(f, stay)]
+    turns = [round((x / (2 * math.pi)) % 1.0 * 2.0 ** 64) % 2 ** 64 for x in f]      # whole turns per position do not show
+    return torch.tensor([t - 2 ** 64 if t >= 2 ** 63 else t for t in turns], dtype=torch.int64, device=device), scale
+
+
+def janus_rope(x: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, *, rot_offset: int = 0, interleaved: bool = False, scale: float = 1.0,
+               inverse: bool = False, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Rotary positions on dims [rot_offset, rot_offset + 2 len(freqs)) of every head.  x [T,H,D] bf16, fp16 or fp32 (dims of a head adjacent, other
+    strides free), positions [T] int64 (negative: padding, the row of `out` stays), freqs from rope_frequencies().  interleaved: neighbouring dims are a
+    pair, else dims half the rotated part apart.  inverse: by the negative angle (the gradient).  Pass out=x to rotate in place."""
+    return _native().rope(x, positions, freqs, rot_offset, interleaved, scale, inverse, out)
+
+
+def janus_rope_append(k: torch.Tensor, v: Optional[torch.Tensor], positions: torch.Tensor, slots: torch.Tensor, freqs: torch.Tensor, k_pool: torch.Tensor,
+                      v_pool: Optional[torch.Tensor], *, rot_offset: int = 0, interleaved: bool = False, scale: float = 1.0,
+                      q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """New rows into the paged cache: keys k [T,n_kv,d_qk] rotated as by janus_rope, values v [T,n_kv,d_v] as they are, to place slots[t] (int64; page *
+    page_size + token, -1: padding) of the pools [n_phys_pages, page_size, n_kv, d].  v and v_pool None: latent rows, whose values are part of the
+    keys.  q [T,H_q,d_qk] is rotated to q_out (allocated if None; q itself: in place) in the same launch; returns q_out.  All bf16."""
+    return _native().rope_append(k, v, positions, slots, freqs, k_pool, v_pool, rot_offset, interleaved, scale, q, q_out)
+
+
+def attn_decode_shared_workspace_size(B: int, H_q: int, d_qk: int, n_kv_heads: int, d_v: int, page_size: int, prefix_len: int, max_len: int) -> int:
+    """Bytes of ``workspace`` that janus_attn_decode_shared asks for."""
+    return int(load().janus_attn_decode_shared_workspace_size(int(B), int(H_q), int(d_qk), int(n_kv_heads), int(d_v), int(page_size), int(prefix_len), int(max_len)))
+
+
+def janus_attn_decode_shared(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor, *, prefix_table: Optional[torch.Tensor], prefix_len: int,
+                             page_tables: Optional[torch.Tensor], table_offsets: Optional[torch.Tensor], kv_lens: torch.Tensor, max_len: int, page_size: int,
+                             softmax_scale: float, d_v: int, want_lse: bool = True, out: Optional[torch.Tensor] = None,
+                             workspace: Optional[torch.Tensor] = None):
+    """Dense attention of one query token per session, q [B,H_q,d_qk] bf16, over the first prefix_len tokens, which all sessions share (pages
+    prefix_table), and the session's own tokens behind them (page_tables / table_offsets of the whole sessions, as janus_batch_plan makes them).
+    kv_lens [B] int64: whole lengths, 0 for an entry that stands empty; max_len bounds them.  Pools [n_phys_pages, page_size, n_kv_heads, d] bf16 (v_pool may
+    be k_pool itself).  Returns (out [B,H_q,d_v] bf16, lse [B,H_q] fp32 | None).  `workspace` (uint8 CUDA tensor) is allocated if not given or too small."""
+    return _native().attn_decode_shared(q, k_pool, v_pool, prefix_table, prefix_len, page_tables, table_offsets, kv_lens, max_len, page_size, softmax_scale, d_v,
+                                        want_lse, out, workspace)
 
 
 # ---- diagnostics ---------------------------------------------------------------------------------------------------

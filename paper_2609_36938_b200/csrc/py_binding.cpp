@@ -15,6 +15,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <exception>
+#include <initializer_list>
 #include <string>
 #include <vector>
 
@@ -41,12 +42,18 @@ struct Api {
     decltype(&janus_topk_batch) topk_batch;
     decltype(&janus_page_demand_batch) page_demand_batch;
     decltype(&janus_sparse_attn_decode) sparse_attn_decode;
+    decltype(&janus_batch_plan) batch_plan;
+    decltype(&janus_rope) rope;
+    decltype(&janus_rope_append) rope_append;
+    decltype(&janus_attn_decode_shared_workspace_size) attn_decode_shared_workspace_size;
+    decltype(&janus_attn_decode_shared) attn_decode_shared;
     decltype(&janus_last_cuda_error) last_cuda_error;
 } api;
 PyObject* janus_error = nullptr;        // exception class
 PyObject* status_tensor_fn = nullptr;   // binding.dev_status_tensor
 auto& status_words = *new std::vector<at::Tensor>;   // by device, as binding.dev_status_tensor made them; never destroyed (outlives CUDA's own teardown)
 PyObject *key_bitmap, *key_pages, *key_runs, *key_counts, *key_miss_pages, *key_miss_runs;
+PyObject *key_row_offsets, *key_kv_lens, *key_table_offsets, *key_page_tables, *key_row_sessions, *key_positions, *key_slots, *key_key_rows;
 
 struct PyError {};                      // a Python exception is set
 [[noreturn]] void fail(PyObject* type, const std::string& what) {
@@ -369,6 +376,176 @@ PyObject* topk_batch(Args a) {        // scores, row_offsets, k, row_lengths, wa
     return triple(wrap(idx), count, kth);
 }
 
+// ---- a step's plan, rotary positions and the cache, dense layers
+void want(bool ok, const char* what) {
+    if (!ok) fail(janus_error, what);
+}
+// One axis of the given type, elements adjacent, on the device; at least n of them (n < 0: any number).
+template <class T>
+T* vec(const at::Tensor& t, at::ScalarType type, int64_t n, const char* name) {
+    if (t.scalar_type() != type || !t.is_contiguous() || t.numel() < n)
+        fail(janus_error, std::string(name) + " must be a contiguous " + c10::toString(type) + " tensor" + (n >= 0 ? " of at least " + std::to_string(n) + " elements" : ""));
+    return as<T>(ptr(t));
+}
+// Tensors whose memory lies on the current device, whose stream and status word the call takes.
+void here(std::initializer_list<const at::Tensor*> list) {
+    for (const at::Tensor* t : list)
+        if (t->defined()) {
+            ptr(*t);      // (refuses host tensors before the device is asked for)
+            if (t->get_device() != c10::cuda::current_device()) fail(janus_error, "a tensor is not on the current device");
+        }
+}
+int32_t* i32_vec(const at::Tensor& t, int64_t n, const char* name) { return vec<int32_t>(t, at::kInt, n, name); }
+int64_t* i64_vec(const at::Tensor& t, int64_t n, const char* name) { return vec<int64_t>(t, at::kLong, n, name); }
+at::Tensor optional(PyObject* o) { return o == Py_None ? at::Tensor() : tensor(o); }
+// int arguments: what does not fit is refused, not cut
+int small(PyObject* o, const char* name) {
+    const int64_t v = size(o);
+    if (v < INT32_MIN || v > INT32_MAX) fail(PyExc_OverflowError, std::string(name) + " is out of range");
+    return static_cast<int>(v);
+}
+
+PyObject* batch_plan(Args a) {        // cached_lens, new_lens, block_tables, free_pages, page_size, n_phys_pages, max_rows, key_offsets, out
+    const at::Tensor &cached = tensor(a[0]), &fresh = tensor(a[1]), &tables = tensor(a[2]), &free_pages = tensor(a[3]), key_offsets = optional(a[7]);
+    want_dims(cached, 1, "cached_lens");
+    want_dims(tables, 2, "block_tables");
+    const int64_t n = cached.numel(), max_rows = size(a[6]);
+    want(fresh.numel() == n && tables.size(0) == n, "cached_lens, new_lens and block_tables must agree in the number of sessions");
+    want(tables.scalar_type() == at::kInt && (tables.size(1) <= 1 || tables.stride(1) == 1), "block_tables must be int32 with adjacent columns");
+    at::Tensor row_offsets, kv_lens, table_offsets, page_tables, row_sessions, positions, slots, counts, key_rows;
+    item(a[8], key_row_offsets, row_offsets); item(a[8], key_kv_lens, kv_lens); item(a[8], key_table_offsets, table_offsets);
+    item(a[8], key_page_tables, page_tables); item(a[8], key_row_sessions, row_sessions); item(a[8], key_positions, positions);
+    item(a[8], key_slots, slots); item(a[8], key_counts, counts);
+    if (key_offsets.defined()) item(a[8], key_key_rows, key_rows);
+    want(n <= INT32_MAX, "too many sessions");
+    auto of = [](const at::Tensor& t, int64_t least, const char* name) { return t.defined() ? i64_vec(t, least, name) : nullptr; };
+    const int64_t *cached_p = of(cached, n, "cached_lens"), *fresh_p = of(fresh, n, "new_lens"), *key_offsets_p = of(key_offsets, n, "key_offsets");
+    int64_t *row_offsets_p = of(row_offsets, n + 1, "row_offsets"), *kv_lens_p = of(kv_lens, n, "kv_lens"), *table_offsets_p = of(table_offsets, n + 1, "table_offsets");
+    int64_t *positions_p = of(positions, max_rows, "positions"), *slots_p = of(slots, max_rows, "slots"), *key_rows_p = of(key_rows, max_rows, "key_rows");
+    int64_t* counts_p = of(counts, 3, "counts");
+    const int32_t* free_p = i32_vec(free_pages, -1, "free_pages");
+    int32_t *page_tables_p = i32_vec(page_tables, -1, "page_tables"), *row_sessions_p = i32_vec(row_sessions, max_rows, "row_sessions");
+    here({&cached, &fresh, &tables, &free_pages, &key_offsets, &row_offsets, &kv_lens, &table_offsets, &page_tables, &row_sessions, &positions, &slots, &counts, &key_rows});
+    call("janus_batch_plan", api.batch_plan, cached_p, fresh_p, i32(n), small(a[4], "page_size"), as<int32_t>(ptr(tables)),
+         n > 1 ? tables.stride(0) : tables.size(1), tables.size(1), free_p, free_pages.numel(), size(a[5]), key_offsets_p, row_offsets_p, kv_lens_p, table_offsets_p,
+         page_tables_p, page_tables.numel(), row_sessions_p, positions_p, slots_p, key_rows_p, max_rows, counts_p, status_word(), stream());
+    return Py_NewRef(a[8]);
+}
+
+int elem_code(const at::Tensor& t, const char* name) {
+    switch (t.scalar_type()) {
+        case at::kBFloat16: return JANUS_ELEM_BF16;
+        case at::kHalf: return JANUS_ELEM_FP16;
+        case at::kFloat: return JANUS_ELEM_FP32;
+        default: fail(janus_error, std::string(name) + " must be bfloat16, float16 or float32, got " + c10::toString(t.scalar_type()));
+    }
+}
+void rows_of_heads(const at::Tensor& t, const char* name) {
+    want_dims(t, 3, name);
+    if (t.size(2) > 1 && t.stride(2) != 1) fail(janus_error, std::string(name) + ": the dims of a head must be adjacent");
+}
+// A tensor with `like`'s shape and type, its dims of a head adjacent.
+bool same_form(const at::Tensor& t, const at::Tensor& like) { return t.sizes() == like.sizes() && t.scalar_type() == like.scalar_type(); }
+
+PyObject* rope(Args a) {              // x, positions, freqs, rot_offset, interleaved, scale, inverse, out
+    const at::Tensor &x = tensor(a[0]), &positions = tensor(a[1]), &freqs = tensor(a[2]);
+    rows_of_heads(x, "x");
+    const int type = elem_code(x, "x");
+    at::Tensor out = a[7] == Py_None ? make(x.sizes(), x.scalar_type(), x) : tensor(a[7]);
+    rows_of_heads(out, "out");
+    want(same_form(out, x), "out must have x's shape and type");
+    const int64_t *positions_p = i64_vec(positions, x.size(0), "positions"), *freqs_p = i64_vec(freqs, 1, "freqs");
+    here({&x, &positions, &freqs, &out});
+    call("janus_rope", api.rope, ptr(x), x.stride(0), x.stride(1), x.size(0), i32(x.size(1)), i32(x.size(2)), positions_p, reinterpret_cast<const uint64_t*>(freqs_p), small(a[3], "rot_offset"), i32(2 * freqs.numel()), i32(truth(a[4])), static_cast<float>(number(a[5])),
+         i32(truth(a[6])), type, ptr(out), out.stride(0), out.stride(1), stream());
+    return a[7] == Py_None ? wrap(out) : Py_NewRef(a[7]);
+}
+
+void bf16(const at::Tensor& t, const char* name) {
+    if (t.scalar_type() != at::kBFloat16) fail(janus_error, std::string(name) + " must be bfloat16, got " + c10::toString(t.scalar_type()));
+}
+void pool_of_rows(const at::Tensor& t, const char* name) {
+    want_dims(t, 4, name);
+    bf16(t, name);
+    if (t.size(3) > 1 && t.stride(3) != 1) fail(janus_error, std::string(name) + ": the dims of a row must be adjacent");
+}
+
+// k, v, positions, slots, freqs, k_pool, v_pool, rot_offset, interleaved, scale, q, q_out
+PyObject* rope_append(Args a) {
+    const at::Tensor &k = tensor(a[0]), &positions = tensor(a[2]), &slots = tensor(a[3]), &freqs = tensor(a[4]), &kp = tensor(a[5]);
+    const at::Tensor v = optional(a[1]), vp = optional(a[6]), q = optional(a[10]);
+    rows_of_heads(k, "k");
+    bf16(k, "k");
+    pool_of_rows(kp, "k_pool");
+    want(v.defined() == vp.defined(), "v and v_pool go together");
+    want(kp.size(2) == k.size(1) && kp.size(3) == k.size(2), "k and k_pool must agree in heads and dims");
+    const int64_t T = k.size(0), d_qk = k.size(2);
+    if (v.defined()) {
+        rows_of_heads(v, "v");
+        bf16(v, "v");
+        pool_of_rows(vp, "v_pool");
+        want(v.size(0) == T && v.size(1) == k.size(1), "k and v must agree in rows and heads");
+        want(vp.size(0) == kp.size(0) && vp.size(1) == kp.size(1) && vp.size(2) == v.size(1) && vp.size(3) == v.size(2), "v_pool must have k_pool's pages and v's heads and dims");
+    }
+    at::Tensor q_out;
+    if (q.defined()) {
+        rows_of_heads(q, "q");
+        bf16(q, "q");
+        want(q.size(0) == T && q.size(2) == d_qk, "q and k must agree in rows and dims");
+        q_out = a[11] == Py_None ? make(q.sizes(), at::kBFloat16, q) : tensor(a[11]);
+        rows_of_heads(q_out, "q_out");
+        want(same_form(q_out, q), "q_out must have q's shape and type");
+    } else {
+        want(a[11] == Py_None, "q_out goes with q");
+    }
+    const int64_t *positions_p = i64_vec(positions, T, "positions"), *slots_p = i64_vec(slots, T, "slots"), *freqs_p = i64_vec(freqs, 1, "freqs");
+    here({&k, &v, &positions, &slots, &freqs, &kp, &vp, &q, &q_out});
+    auto at_ = [](const at::Tensor& t) { return t.defined() ? ptr(t) : nullptr; };
+    auto st = [](const at::Tensor& t, int d) { return t.defined() ? t.stride(d) : int64_t(0); };
+    call("janus_rope_append", api.rope_append, at_(q), st(q, 0), st(q, 1), q.defined() ? i32(q.size(1)) : 0, ptr(k), k.stride(0), k.stride(1), i32(k.size(1)),
+         i32(d_qk), at_(v), st(v, 0), st(v, 1), v.defined() ? i32(v.size(2)) : 0, T, positions_p, slots_p,
+         reinterpret_cast<const uint64_t*>(freqs_p), small(a[7], "rot_offset"), i32(2 * freqs.numel()), i32(truth(a[8])), static_cast<float>(number(a[9])),
+         at_(q_out), st(q_out, 0), st(q_out, 1), ptr(kp), kp.stride(0), kp.stride(1), kp.stride(2), at_(vp), st(vp, 0), st(vp, 1), st(vp, 2), i32(kp.size(1)),
+         kp.size(0), status_word(), stream());
+    if (!q.defined()) return none();
+    return a[11] == Py_None ? wrap(q_out) : Py_NewRef(a[11]);
+}
+
+// q, k_pool, v_pool, prefix_table, prefix_len, page_tables, table_offsets, kv_lens, max_len, page_size, softmax_scale, d_v, want_lse, out, workspace
+PyObject* attn_decode_shared(Args a) {
+    const at::Tensor &q = tensor(a[0]), &kp = tensor(a[1]), &vp = tensor(a[2]), &lens = tensor(a[7]);
+    const at::Tensor prefix = optional(a[3]), tables = optional(a[5]), offsets = optional(a[6]);
+    want_dims(q, 3, "q");
+    bf16(q, "q");
+    pool_of_rows(kp, "k_pool");
+    pool_of_rows(vp, "v_pool");
+    const int64_t n = q.size(0), H = q.size(1), d_qk = q.size(2), n_kv = kp.size(2), d_v = size(a[11]), prefix_len = size(a[4]), max_len = size(a[8]);
+    const int page = small(a[9], "page_size");
+    want(q.is_contiguous(), "q must be contiguous");
+    want(kp.size(1) == page && vp.size(1) == page && vp.size(0) == kp.size(0) && vp.size(2) == n_kv, "the pools must be [pages, page_size, kv heads, dims], both of the same pages");
+    want(kp.size(3) == d_qk && vp.size(3) >= d_v && d_v > 0, "the rows of the pools are shorter than the heads");
+    want(prefix_len >= 0 && page > 0, "prefix_len must not be negative, page_size is positive");
+    if (prefix_len > 0 && (!prefix.defined() || prefix.numel() < (prefix_len + page - 1) / page)) fail(janus_error, "prefix_table must cover prefix_len tokens");
+    at::Tensor out = a[13] == Py_None ? make({n, H, d_v}, at::kBFloat16, q) : tensor(a[13]), lse;
+    want(out.sizes() == at::IntArrayRef({n, H, d_v}) && out.scalar_type() == at::kBFloat16 && out.is_contiguous(), "out must be a contiguous [B, H_q, d_v] bfloat16 tensor");
+    if (truth(a[12])) lse = make({n, H}, at::kFloat, q);
+    const size_t need = api.attn_decode_shared_workspace_size(i32(n), i32(H), i32(d_qk), i32(n_kv), i32(d_v), page, prefix_len, max_len);
+    at::Tensor ws = optional(a[14]);
+    if (ws.defined()) want(ws.scalar_type() == at::kByte && ws.is_contiguous(), "workspace must be a contiguous uint8 tensor");
+    if (!ws.defined() || ws.numel() < static_cast<int64_t>(need)) ws = make({static_cast<int64_t>(need > 16 ? need : 16)}, at::kByte, q);
+    const int32_t *prefix_p = prefix.defined() ? i32_vec(prefix, -1, "prefix_table") : nullptr, *tables_p = tables.defined() ? i32_vec(tables, -1, "page_tables") : nullptr;
+    const int64_t *offsets_p = offsets.defined() ? i64_vec(offsets, n + 1, "table_offsets") : nullptr, *lens_p = i64_vec(lens, n, "kv_lens");
+    here({&q, &kp, &vp, &lens, &prefix, &tables, &offsets, &out, &ws});
+    call("janus_attn_decode_shared", api.attn_decode_shared, ptr(q), i32(n), i32(H), i32(d_qk), ptr(kp), kp.stride(0), kp.stride(1), kp.stride(2), ptr(vp), vp.stride(0),
+         vp.stride(1), vp.stride(2), i32(n_kv), i32(d_v), page, kp.size(0), prefix_p, prefix_len, tables_p, offsets_p,
+         lens_p, max_len, static_cast<float>(number(a[10])), ptr(out), lse.defined() ? as<float>(ptr(lse)) : nullptr, ptr(ws),
+         static_cast<size_t>(ws.numel()), status_word(), stream());
+    PyObject* t = PyTuple_New(2);
+    PyTuple_SET_ITEM(t, 0, a[13] == Py_None ? wrap(out) : Py_NewRef(a[13]));
+    PyTuple_SET_ITEM(t, 1, lse.defined() ? wrap(lse) : none());
+    return t;
+}
+
 // ---- module
 template <PyObject* (*F)(Args), int N>
 PyObject* entry(PyObject*, Args args, Py_ssize_t n) {
@@ -416,6 +593,11 @@ PyObject* init(PyObject*, Args args, Py_ssize_t n) {      // path of libjanus.so
     find(api.topk_batch, "janus_topk_batch");
     find(api.page_demand_batch, "janus_page_demand_batch");
     find(api.sparse_attn_decode, "janus_sparse_attn_decode");
+    find(api.batch_plan, "janus_batch_plan");
+    find(api.rope, "janus_rope");
+    find(api.rope_append, "janus_rope_append");
+    find(api.attn_decode_shared_workspace_size, "janus_attn_decode_shared_workspace_size");
+    find(api.attn_decode_shared, "janus_attn_decode_shared");
     find(api.last_cuda_error, "janus_last_cuda_error");
     if (!ok) {
         PyErr_SetString(args[1], "libjanus.so lacks an entry point");
@@ -441,6 +623,10 @@ PyMethodDef methods[] = {
     JANUS_METHOD(entry_expand, 3),
     JANUS_METHOD(indexer_scores_batch, 11),
     JANUS_METHOD(topk_batch, 6),
+    JANUS_METHOD(batch_plan, 9),
+    JANUS_METHOD(rope, 8),
+    JANUS_METHOD(rope_append, 12),
+    JANUS_METHOD(attn_decode_shared, 15),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
@@ -454,5 +640,13 @@ PyMODINIT_FUNC PyInit__native() {
     key_counts = PyUnicode_InternFromString("counts");
     key_miss_pages = PyUnicode_InternFromString("miss_pages");
     key_miss_runs = PyUnicode_InternFromString("miss_runs");
+    key_row_offsets = PyUnicode_InternFromString("row_offsets");
+    key_kv_lens = PyUnicode_InternFromString("kv_lens");
+    key_table_offsets = PyUnicode_InternFromString("table_offsets");
+    key_page_tables = PyUnicode_InternFromString("page_tables");
+    key_row_sessions = PyUnicode_InternFromString("row_sessions");
+    key_positions = PyUnicode_InternFromString("positions");
+    key_slots = PyUnicode_InternFromString("slots");
+    key_key_rows = PyUnicode_InternFromString("key_rows");
     return PyModule_Create(&module);
 }

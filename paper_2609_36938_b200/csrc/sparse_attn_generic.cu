@@ -15,6 +15,7 @@ template <int G>
 __global__ void __launch_bounds__(AG_THREADS)
 sparse_attn_generic_kernel(const uint16_t* q, int M, int H_q, int d_qk, const uint16_t* k_pool,
                            const uint16_t* v_pool, int64_t page_stride, int64_t tok_stride, int64_t head_stride,
+                           int64_t v_page_stride, int64_t v_tok_stride, int64_t v_head_stride,
                            int n_kv_heads, int d_v, const int32_t* idx, int k, int page_size,
                            const int32_t* page_table, int64_t n_logical_pages, const int64_t* table_offsets,
                            float softmax_scale, uint16_t* __restrict__ out, float* __restrict__ lse, int32_t* dev_status) {
@@ -74,13 +75,13 @@ sparse_attn_generic_kernel(const uint16_t* q, int M, int H_q, int d_qk, const ui
         for (int r = warp; r < AG_KT; r += AG_THREADS / 32) {
             const int s = srow[r];
             if (s < 0) continue;
-            const int64_t off = static_cast<int64_t>(ld_input(page_table + s / page_size)) * page_stride +
-                                static_cast<int64_t>(s % page_size) * tok_stride + static_cast<int64_t>(hk) * head_stride;
+            const int64_t page = ld_input(page_table + s / page_size), within = s % page_size;
+            const int64_t off = page * page_stride + within * tok_stride + static_cast<int64_t>(hk) * head_stride;
             const uint4* src = reinterpret_cast<const uint4*>(k_pool + off);
             uint4* dst = reinterpret_cast<uint4*>(ks + r * kpad);
             for (int c = lane; c < d_qk / 8; c += 32) dst[c] = ld_input(src + c);
             if (!v_alias) {
-                const uint4* vsrc = reinterpret_cast<const uint4*>(v_pool + off);
+                const uint4* vsrc = reinterpret_cast<const uint4*>(v_pool + page * v_page_stride + within * v_tok_stride + static_cast<int64_t>(hk) * v_head_stride);
                 uint4* vdst = reinterpret_cast<uint4*>(vs + r * vpad);
                 for (int c = lane; c < d_v / 8; c += 32) vdst[c] = ld_input(vsrc + c);
             }
@@ -170,7 +171,8 @@ sparse_attn_generic_kernel(const uint16_t* q, int M, int H_q, int d_qk, const ui
 
 template <int G>
 static int launch_g(const void* q, int M, int H_q, int d_qk, const void* k_pool, const void* v_pool, int64_t page_stride,
-                    int64_t tok_stride, int64_t head_stride, int n_kv_heads, int d_v, const int32_t* idx, int k, int page_size,
+                    int64_t tok_stride, int64_t head_stride, int64_t v_page_stride, int64_t v_tok_stride, int64_t v_head_stride, int n_kv_heads, int d_v,
+                    const int32_t* idx, int k, int page_size,
                     const int32_t* page_table, int64_t n_logical_pages, const int64_t* table_offsets, float softmax_scale, void* out,
                     float* lse, int32_t* dev_status, cudaStream_t stream) {
     const bool v_alias = (v_pool == k_pool);
@@ -183,17 +185,19 @@ static int launch_g(const void* q, int M, int H_q, int d_qk, const void* k_pool,
     dim3 grid(M, n_kv_heads * ((heads_per_kv + G - 1) / G));
     JANUS_CUDA_CHECK(launch_kernel(sparse_attn_generic_kernel<G>, grid, AG_THREADS, smem, stream, 1, static_cast<const uint16_t*>(q), M, H_q, d_qk,
                                    static_cast<const uint16_t*>(k_pool), static_cast<const uint16_t*>(v_pool), page_stride, tok_stride, head_stride,
+                                   v_page_stride, v_tok_stride, v_head_stride,
                                    n_kv_heads, d_v, idx, k, page_size, page_table, n_logical_pages, table_offsets, softmax_scale,
                                    static_cast<uint16_t*>(out), lse, dev_status));
     return JANUS_OK;
 }
 
 int launch_sparse_attn_generic(const void* q, int M, int H_q, int d_qk, const void* k_pool, const void* v_pool, int64_t page_stride,
-                               int64_t tok_stride, int64_t head_stride, int n_kv_heads, int d_v, const int32_t* idx, int k,
+                               int64_t tok_stride, int64_t head_stride, int64_t v_page_stride, int64_t v_tok_stride, int64_t v_head_stride, int n_kv_heads,
+                               int d_v, const int32_t* idx, int k,
                                int page_size, const int32_t* page_table, int64_t n_logical_pages, const int64_t* table_offsets,
                                float softmax_scale, void* out, float* lse, int32_t* dev_status, cudaStream_t stream) {
     const int heads_per_kv = H_q / n_kv_heads;
-#define JANUS_AG_ARGS q, M, H_q, d_qk, k_pool, v_pool, page_stride, tok_stride, head_stride, n_kv_heads, d_v, idx, k, page_size, \
+#define JANUS_AG_ARGS q, M, H_q, d_qk, k_pool, v_pool, page_stride, tok_stride, head_stride, v_page_stride, v_tok_stride, v_head_stride, n_kv_heads, d_v, idx, k, page_size, \
                       page_table, n_logical_pages, table_offsets, softmax_scale, out, lse, dev_status, stream
     if (heads_per_kv >= 8) return launch_g<8>(JANUS_AG_ARGS);
     if (heads_per_kv >= 4) return launch_g<4>(JANUS_AG_ARGS);

@@ -208,7 +208,8 @@ __device__ __forceinline__ void lp_merge_splits(const LpParams& p, int t, int s,
 // SPLIT = false: clusters of two CTAs, persistent over tokens.  SPLIT = true: a cluster of 2 n CTAs takes one token, pair s of it
 // the tiles [s, s + 1) * n_tiles / n, and the pairs' outputs are merged through distributed shared memory at the end.
 // ROWS = true: the pool's rows lie at whole multiples of one stride and those of K are gathered by number; false: by address.
-template <bool SPLIT, bool ROWS>
+// EXACT_SUM = true: the row sum adds the probabilities before they are rounded (below).
+template <bool SPLIT, bool ROWS, bool EXACT_SUM>
 __global__ void __launch_bounds__(LP_THREADS, 1) sparse_attn_latent_pair_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_pool,
                                                                               const LpParams p) {
     extern __shared__ __align__(1024) unsigned char smem[];
@@ -691,15 +692,16 @@ __global__ void __launch_bounds__(LP_THREADS, 1) sparse_attn_latent_pair_kernel(
             }
             const float neg_m = (m_ref == neg_inf) ? 0.f : -m_ref;
             // P is rounded to bf16 (one pack instruction per pair); the row sum adds the very same rounded values, so the
-            // normalisation stays consistent and the log-sum-exp is not biased
+            // normalisation stays consistent and the log-sum-exp is not biased.  With EXACT_SUM it adds them as they were: over all tokens of a
+            // session the rounding of single probabilities leaves 3e-5 in the log-sum-exp, and in the output what its own rounding hides.
             uint32_t pk[16];
             float2 ts[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
             const float2 sc2 = make_float2(p.scale_log2e, p.scale_log2e), nm2 = make_float2(neg_m, neg_m);
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
-                const float2 e = ffma2(x[j], sc2, nm2);
-                pk[j] = lp_pack_bf16x2(lp_exp2(e.x), lp_exp2(e.y));       // low half = bf16(p of key 2j), high half = bf16(p of key 2j+1)
-                ts[j & 3] = fadd2(ts[j & 3], make_float2(__uint_as_float(pk[j] << 16), __uint_as_float(pk[j] & 0xffff0000u)));
+                const float2 e = ffma2(x[j], sc2, nm2), pr = make_float2(lp_exp2(e.x), lp_exp2(e.y));
+                pk[j] = lp_pack_bf16x2(pr.x, pr.y);       // low half = bf16(p of key 2j), high half = bf16(p of key 2j+1)
+                ts[j & 3] = fadd2(ts[j & 3], EXACT_SUM ? pr : make_float2(__uint_as_float(pk[j] << 16), __uint_as_float(pk[j] & 0xffff0000u)));
             }
             const float2 t4 = fadd2(fadd2(ts[0], ts[1]), fadd2(ts[2], ts[3]));
             l_sum += t4.x + t4.y;
@@ -797,12 +799,18 @@ static int lp_resident_clusters(int dev, size_t smem, int (&n)[LP_MAX_SPLIT + 1]
         cudaError_t e = cudaSuccess;
         auto larger = [&](auto kernel) { if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); };
         auto wider = [&](auto kernel) { if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1); };
-        larger(sparse_attn_latent_pair_kernel<false, false>);
-        larger(sparse_attn_latent_pair_kernel<false, true>);
-        larger(sparse_attn_latent_pair_kernel<true, false>);
-        larger(sparse_attn_latent_pair_kernel<true, true>);
-        wider(sparse_attn_latent_pair_kernel<true, false>);
-        wider(sparse_attn_latent_pair_kernel<true, true>);
+        larger(sparse_attn_latent_pair_kernel<false, false, false>);
+        larger(sparse_attn_latent_pair_kernel<false, true, false>);
+        larger(sparse_attn_latent_pair_kernel<true, false, false>);
+        larger(sparse_attn_latent_pair_kernel<true, true, false>);
+        larger(sparse_attn_latent_pair_kernel<false, false, true>);
+        larger(sparse_attn_latent_pair_kernel<false, true, true>);
+        larger(sparse_attn_latent_pair_kernel<true, false, true>);
+        larger(sparse_attn_latent_pair_kernel<true, true, true>);
+        wider(sparse_attn_latent_pair_kernel<true, false, false>);
+        wider(sparse_attn_latent_pair_kernel<true, true, false>);
+        wider(sparse_attn_latent_pair_kernel<true, false, true>);
+        wider(sparse_attn_latent_pair_kernel<true, true, true>);
         return e;
     }));
     std::lock_guard<std::mutex> lock(mu);
@@ -811,8 +819,8 @@ static int lp_resident_clusters(int dev, size_t smem, int (&n)[LP_MAX_SPLIT + 1]
         for (int s = LP_MAX_SPLIT; s >= 1; --s) {
             cudaLaunchAttribute attr;
             const cudaLaunchConfig_t cfg = lp_occupancy_config(2 * s, 148, smem, &attr);
-            const cudaError_t e = s > 1 ? cudaOccupancyMaxActiveClusters(&k[s], sparse_attn_latent_pair_kernel<true, true>, &cfg)
-                                        : cudaOccupancyMaxActiveClusters(&k[s], sparse_attn_latent_pair_kernel<false, true>, &cfg);
+            const cudaError_t e = s > 1 ? cudaOccupancyMaxActiveClusters(&k[s], sparse_attn_latent_pair_kernel<true, true, false>, &cfg)
+                                        : cudaOccupancyMaxActiveClusters(&k[s], sparse_attn_latent_pair_kernel<false, true, false>, &cfg);
             if (e != cudaSuccess) {
                 (void)cudaGetLastError();
                 k[s] = 0;
@@ -830,7 +838,7 @@ static int lp_resident_clusters(int dev, size_t smem, int (&n)[LP_MAX_SPLIT + 1]
 
 int launch_sparse_attn_latent_tc(const void* q, int M, const void* pool, int64_t page_stride, int64_t tok_stride, const int32_t* idx, int k,
                                  int page_size, const int32_t* page_table, int64_t n_logical_pages, const int64_t* table_offsets,
-                                 float softmax_scale, void* out, float* lse, int32_t* dev_status, cudaStream_t stream) {
+                                 float softmax_scale, void* out, float* lse, int32_t* dev_status, cudaStream_t stream, bool exact_sum) {
     LpParams p;
     p.q = static_cast<const uint16_t*>(q);
     p.pool = static_cast<const uint16_t*>(pool);
@@ -883,11 +891,13 @@ int launch_sparse_attn_latent_tc(const void* q, int M, const void* pool, int64_t
     const bool rows = page_stride >= 0 && page_stride % tok_stride == 0 &&
                       make_tmap_2d_sw128(&map, pool, 2, 0x7fffffffu, LP_DQK, static_cast<uint64_t>(tok_stride) * 2, 1, 64);
     const int cluster = 2 * split;
-    cudaError_t e;
-    if (split > 1) e = rows ? launch_kernel(sparse_attn_latent_pair_kernel<true, true>, grid, LP_THREADS, smem, stream, cluster, map_q, map, p)
-                            : launch_kernel(sparse_attn_latent_pair_kernel<true, false>, grid, LP_THREADS, smem, stream, cluster, map_q, map, p);
-    else e = rows ? launch_kernel(sparse_attn_latent_pair_kernel<false, true>, grid, LP_THREADS, smem, stream, cluster, map_q, map, p)
-                  : launch_kernel(sparse_attn_latent_pair_kernel<false, false>, grid, LP_THREADS, smem, stream, cluster, map_q, map, p);
+    auto launch = [&](auto kernel) { return launch_kernel(kernel, grid, LP_THREADS, smem, stream, cluster, map_q, map, p); };
+    auto pick = [&](auto exact) {
+        constexpr bool E = decltype(exact)::value;
+        if (split > 1) return rows ? launch(sparse_attn_latent_pair_kernel<true, true, E>) : launch(sparse_attn_latent_pair_kernel<true, false, E>);
+        return rows ? launch(sparse_attn_latent_pair_kernel<false, true, E>) : launch(sparse_attn_latent_pair_kernel<false, false, E>);
+    };
+    const cudaError_t e = exact_sum ? pick(std::true_type{}) : pick(std::false_type{});
     JANUS_CUDA_CHECK(e);
     return JANUS_OK;
 }
