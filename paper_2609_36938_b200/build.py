@@ -14,7 +14,7 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libjanus.so")
 NATIVE_PATH = os.path.join(PKG_DIR, "_native.so")
 SOURCES = ["janus_api.cu", "indexer_generic.cu", "indexer_tc.cu", "indexer_tc_batch.cu", "topk.cu", "page_demand.cu", "sparse_attn_generic.cu",
-           "sparse_attn_heads.cu", "sparse_attn_latent_pair.cu", "indexer_topk.cu", "batch_plan.cu", "rope.cu", "attn_shared.cu", "diagnostics.cu"]
+           "sparse_attn_heads.cu", "sparse_attn_latent_pair.cu", "indexer_topk.cu", "batch_plan.cu", "rope.cu", "attn_shared.cu", "attn_shared_tc.cu", "diagnostics.cu"]
 
 
 def _nvcc() -> str:

@@ -5,7 +5,7 @@
 // of the prefix, then its own) and the list of its tokens.  That is the way of layouts whose work is bound by the matrix units for one session
 // already, so that reading the prefix once for all gains nothing (latent: 128 heads read one row per token, 242 flops a byte), and of head
 // dims without a kernel of their own.
-#include "janus_common.cuh"
+#include "attn_shared.cuh"
 
 namespace janus {
 
@@ -87,6 +87,7 @@ static size_t sl_bytes(int B, int page_size, int64_t prefix, int64_t max_len) {
 extern "C" size_t janus_attn_decode_shared_workspace_size(int B, int H_q, int d_qk, int n_kv_heads, int d_v, int page_size, int64_t prefix_len, int64_t max_len) {
     using namespace janus;
     if (B <= 0 || H_q <= 0 || d_qk <= 0 || n_kv_heads <= 0 || d_v <= 0 || page_size <= 0 || prefix_len < 0 || max_len < prefix_len) return 0;
+    if (attn_shared_tc_supported(d_qk, d_v)) return attn_shared_tc_workspace(B, H_q, n_kv_heads, d_v, prefix_len, max_len);
     return sl_bytes(B, page_size, prefix_len, max_len);
 }
 
@@ -107,11 +108,18 @@ extern "C" int janus_attn_decode_shared(const void* q, int B, int H_q, int d_qk,
     if ((prefix_len > 0 && !prefix_table) || (max_len > prefix_len && (!page_tables || !table_offsets))) return JANUS_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(k_pool) || !aligned16(v_pool) || !aligned16(out) || !aligned16(ws)) return JANUS_ERR_INVALID_ARG;
     if (((k_page_stride | k_tok_stride | k_head_stride | v_page_stride | v_tok_stride | v_head_stride) % 8) != 0) return JANUS_ERR_INVALID_ARG;
+    auto positive = [&](int64_t page, int64_t tok, int64_t head) { return (n_phys_pages <= 1 || page > 0) && (page_size <= 1 || tok > 0) && (n_kv_heads <= 1 || head > 0); };
+    if (!positive(k_page_stride, k_tok_stride, k_head_stride) || !positive(v_page_stride, v_tok_stride, v_head_stride)) return JANUS_ERR_INVALID_ARG;
+    if (n_phys_pages == 0 && max_len > 0) return JANUS_ERR_INVALID_ARG;
     const bool same_strides = k_page_stride == v_page_stride && k_tok_stride == v_tok_stride && (n_kv_heads == 1 || k_head_stride == v_head_stride);
     if (v_pool == k_pool && (d_v > d_qk || !same_strides)) return JANUS_ERR_INVALID_ARG;
     if (ws_bytes < janus_attn_decode_shared_workspace_size(B, H_q, d_qk, n_kv_heads, d_v, page_size, prefix_len, max_len)) return JANUS_ERR_WORKSPACE_TOO_SMALL;
     if (!ws) return JANUS_ERR_INVALID_ARG;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    if (attn_shared_tc_supported(d_qk, d_v))
+        return launch_attn_shared_tc({q, B, H_q, d_qk, k_pool, k_page_stride, k_tok_stride, k_head_stride, v_pool, v_page_stride, v_tok_stride, v_head_stride, n_kv_heads,
+                                      d_v, page_size, n_phys_pages, prefix_table, prefix_len, page_tables, table_offsets, kv_lens, max_len, softmax_scale, out, lse, ws,
+                                      dev_status}, stream);
 
     SlParams p;
     p.prefix_table = prefix_table; p.page_tables = page_tables; p.table_offsets = table_offsets; p.kv_lens = kv_lens;
