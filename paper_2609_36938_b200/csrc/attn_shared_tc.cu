@@ -23,6 +23,8 @@
 // The running maximum moves only when a tile exceeds it by more than 2^8, so O is rescaled a handful of times per fragment.  P is rounded to
 // bf16 (half a step, 2^-8 relative, as the output itself); the row sum adds the probabilities as they were, so the log-sum-exp is exact to fp32.
 // Every wait is bounded; on a timeout the CTA reports JANUS_DEV_WAIT_TIMEOUT and leaves when its copies have landed.
+#include <type_traits>
+
 #include "attn_shared.cuh"
 #include "sm100_ptx.cuh"
 
@@ -31,24 +33,50 @@ namespace janus {
 using namespace ptx;
 
 constexpr int ST_ROWS = 128;                        // rows of an MMA
-constexpr int ST_SOFTMAX_WARPS = 8, ST_COPY_WARP = 8, ST_MMA_WARP = 9, ST_THREADS = 320;
+constexpr int ST_SOFTMAX_WARPS = 8, ST_COPY_WARP = 8, ST_QK_WARP = 9, ST_PV_WARP = 10, ST_QUERY_WARP = 11, ST_THREADS = 384;
+constexpr int ST_READERS = ST_SOFTMAX_WARPS + 3;    // warps that fragments are worked out for
 constexpr int ST_INFO = 8;                          // tiles whose masks are kept
 constexpr int ST_MAX_SLOTS = 8;
 static_assert(ST_INFO >= ST_MAX_SLOTS / 2 + 2, "the copying warp is at most so many tiles ahead of a softmax");
 constexpr int ST_MAX_SESSIONS = 1024;               // of one launch: their tile counts lie in shared memory
 constexpr int ST_MAX_CTAS = 148;
+// Tensor memory: O of group w in columns [256 + 128 w, ...).  With more than 128 rows one S, [0, 128), and P of group w in [128 + 64 w, ...): a group
+// takes S into registers at once, so that the next logits are computed while it still works on these.  Else S of group w in [128 w, ...), and P over it.
 constexpr uint32_t ST_COL_O = 256;
+__device__ __forceinline__ uint32_t st_col_s(bool heavy, uint32_t w) { return heavy ? 0u : 128u * w; }
+__device__ __forceinline__ uint32_t st_col_p(bool heavy, uint32_t w) { return heavy ? 128u + 64u * w : 128u * w; }
+
+constexpr int ST_FRAGMENTS = 4;                     // fragments that are worked out ahead
+struct StFragment {
+    int prefix, heavy, last;       // last: there is no further one, and this is none either
+    int h;                 // kv head
+    int c0;                // first chunk
+    int rows;              // of the first 128, of the second
+    int rows2;
+    int b;                 // session (own)
+    int t0, t1;            // tiles of the segment
+    int64_t place;
+};
+
+constexpr int ST_JOIN = 20;                         // floats of a lane: 16 dims and a pad of 16 bytes, or more dims of fewer lanes
 
 struct StShared {
     uint64_t full[ST_MAX_SLOTS], empty[ST_MAX_SLOTS];
     uint64_t info_full[ST_INFO];
-    uint64_t s_full[2], p_full[2], o_done[2];       // by group: logits complete; P written, O rescaled; the fragment's last P . V done
-    uint64_t q_full, drain;
-    uint64_t left;                                  // both groups are through with a fragment
+    uint64_t s_full[2], s_free[2];                  // by group: logits complete; in registers (more than 128 rows)
+    uint64_t p_full[2], pv_done[2];                 // P written, O rescaled; P . V done
+    uint64_t q_full[2], q_empty[2];                 // queries of 128 rows are there / their place is no longer needed
+    uint64_t f_full[ST_FRAGMENTS], f_empty[ST_FRAGMENTS];      // fragment worked out / taken over by the warps that work on it
+    uint64_t pv_all;                                // the fragment's last P . V is done
+    uint64_t meet[2];                               // the warps of a group wait for one another
+    uint64_t drain[2];
     uint32_t partial[ST_INFO];                      // whether some key of the tile does not count
     uint32_t mask[ST_INFO][4];
+    StFragment fragment[ST_FRAGMENTS];
     uint32_t tmem_base, abort;
     int warp_sums[33];
+    float2 ml[2][ST_ROWS];                          // by group: maxima and sums of the copies, to be joined,
+    alignas(16) float join[2][ST_ROWS * ST_JOIN];   // and their outputs, some dims at a time
     int32_t own_base[ST_MAX_SESSIONS + 1];          // tiles of the sessions before, per kv head
 };
 
@@ -61,24 +89,28 @@ struct StShape {
     static constexpr int ROOM = (227 * 1024 - static_cast<int>(sizeof(StShared)) - Q_BYTES) / SLOT;
     static constexpr int SLOTS = ROOM < ST_MAX_SLOTS ? ROOM : ST_MAX_SLOTS;
     static_assert(SLOTS >= 4, "K and V of a tile, and of the next");
+    static constexpr int Q_PLACE = Q_BYTES / 2;
+    static constexpr int COPIES = KT / 32;                            // a row's keys are shared by so many lanes at most
     static constexpr int SMEM = Q_BYTES + SLOTS * SLOT + static_cast<int>(sizeof(StShared));
 };
 
 struct StParams {
     const uint16_t* q;
     int B, H_q, n_kv, group;
-    int own_rows, own_parts;             // rows of an own segment, and how many cover a group
+    // The query heads of a session that share a kv head are a chunk of rows; more than 128 of them are several (parts).  128 rows of a prefix segment
+    // hold so many whole chunks (per_tile).
+    int chunk_rows, parts, per_tile, chunks;
     int page_size, page_shift, box, n_phys;
     const int32_t* prefix_table;
     const int32_t* page_tables;
     const int64_t* table_offsets;
     const int64_t* kv_lens;
     int64_t prefix, own_start, max_len;  // own_start: where the tiles of the own tokens begin, prefix rounded down to a box
-    int64_t prefix_tiles, prefix_units;  // of a segment; of all segments
-    int prefix_segments, heavy_segments; // the first ones have more than 128 rows
+    int prefix_tiles, prefix_units;      // tiles of a segment, units of all segments
+    int heavy_segments;                  // the first ones have more than 128 rows
     float scale_log2e;
-    float *pre_o, *own_o;                // [place][256][d_v], [place][2][own_rows][d_v]
-    float2 *pre_ml, *own_ml;             // maximum and sum, in the same places
+    float *pre_o, *own_o;                // [place][2][d_v / 4][rows][4], rows: 128, chunk_rows
+    float2 *pre_ml, *own_ml;             // [place][2][rows]: maximum and sum
     int32_t* own_base;                   // for the merge
     int n_ctas;
     uint16_t* out;
@@ -86,72 +118,69 @@ struct StParams {
     int32_t* dev_status;
 };
 
-// The line of tiles counts units: two for a tile of more than 128 rows, whose MMAs take twice the time.
-constexpr int ST_HEAVY_UNITS = 2;
+// The line counts units: so many for a tile of more than 128 rows, for one of fewer, and for what a segment costs besides its tiles.
+constexpr int ST_HEAVY = 8, ST_LIGHT = 6, ST_SEGMENT = 10;
 
-struct StFragment {
-    bool prefix, heavy;
-    int h;                 // kv head
-    int row0;              // first row: of all rows (prefix), of the group (own)
-    int rows;
-    int b;                 // session (own)
-    int64_t t0, t1;        // tiles of the segment
-    int64_t place;
-};
+// Lanes that share the keys of a row: where rows are so few that there are lanes for `most` of each, every one takes a slice of a tile's keys, with a
+// maximum, a sum and an output of its own until the fragment ends.  Lane i holds copy i / (128 / copies), row i % (128 / copies).
+__device__ __forceinline__ int st_copies(bool heavy, int rows, int most) { return !heavy && rows <= ST_ROWS / most ? most : 1; }
 
-// First tile of a segment of `w` units a tile that belongs to the stretch from unit u on; u0: the segment's first unit.
-__device__ __forceinline__ int64_t st_tile(int64_t u, int64_t u0, int w) { return (u - u0 + w - 1) / w; }
+__device__ __forceinline__ int st_units(int tiles, int w) { return tiles * w + ST_SEGMENT; }
+// Tiles of a segment that begin before its unit x.
+__device__ __forceinline__ int st_tiles(int x, int w) { return x <= ST_SEGMENT ? 0 : (x - ST_SEGMENT + w - 1) / w; }
 
-__device__ __forceinline__ void st_prefix_segment(const StParams& p, int s, int64_t& u0, int& w) {
-    const int64_t heavy_units = p.prefix_tiles * ST_HEAVY_UNITS;
-    w = s < p.heavy_segments ? ST_HEAVY_UNITS : 1;
-    u0 = s < p.heavy_segments ? s * heavy_units : p.heavy_segments * heavy_units + (s - p.heavy_segments) * p.prefix_tiles;
+// First unit of prefix segment s, and the units of its tiles.
+__device__ __forceinline__ int st_prefix_segment(const StParams& p, int s, int& w) {
+    const int heavy = st_units(p.prefix_tiles, ST_HEAVY), light = st_units(p.prefix_tiles, ST_LIGHT);
+    w = s < p.heavy_segments ? ST_HEAVY : ST_LIGHT;
+    return s < p.heavy_segments ? s * heavy : p.heavy_segments * heavy + (s - p.heavy_segments) * light;
 }
 
-// Next fragment of the stretch [u, end) of CTA `cta`; false when there is none.
-__device__ __forceinline__ bool st_next(const StParams& p, const int32_t* own_base, int cta, int64_t& u, int64_t end, StFragment& f) {
-    while (u < end) {
+// Units that a CTA takes of `units` in all.
+__device__ __forceinline__ int st_share(const StParams& p, int units) { return units > p.n_ctas ? (units - 1) / p.n_ctas + 1 : 1; }
+
+// Next fragment of the stretch [u, end) of CTA `cta`; false when there is none.  It may be without a tile (none of the segment begins in the stretch).
+__device__ __forceinline__ bool st_next(const StParams& p, const int32_t* own_base, int cta, int& u, int end, StFragment& f) {
+    if (u < end) {
+        int u0, w, tiles;
         if (u < p.prefix_units) {
-            const int64_t heavy_units = p.prefix_tiles * ST_HEAVY_UNITS, all_heavy = p.heavy_segments * heavy_units;
-            const int s = static_cast<int>(u < all_heavy ? u / heavy_units : p.heavy_segments + (u - all_heavy) / p.prefix_tiles);
-            int64_t u0;
-            int w;
-            st_prefix_segment(p, s, u0, w);
-            const int64_t u1 = u0 + w * p.prefix_tiles, stop = end < u1 ? end : u1;
+            const int heavy = st_units(p.prefix_tiles, ST_HEAVY), all_heavy = p.heavy_segments * heavy;
+            const int s = u < all_heavy ? u / heavy : p.heavy_segments + (u - all_heavy) / st_units(p.prefix_tiles, ST_LIGHT);
+            u0 = st_prefix_segment(p, s, w);
+            tiles = p.prefix_tiles;
             f.prefix = true;
-            f.heavy = w == ST_HEAVY_UNITS;
+            f.heavy = s < p.heavy_segments;
             f.h = s % p.n_kv;
-            f.row0 = s / p.n_kv * 2 * ST_ROWS;
-            f.rows = min(2 * ST_ROWS, p.B * p.group - f.row0);
+            f.c0 = s / p.n_kv * 2 * p.per_tile;
+            f.rows = min(p.per_tile, p.chunks - f.c0) * p.chunk_rows;
+            f.rows2 = f.heavy ? min(p.per_tile, p.chunks - f.c0 - p.per_tile) * p.chunk_rows : 0;
             f.b = 0;
-            f.t0 = st_tile(u, u0, w);
-            f.t1 = st_tile(stop, u0, w);
             f.place = static_cast<int64_t>(cta) + s;
-            u = stop;
-            if (f.t0 < f.t1) return true;
         } else {
-            const int parts = p.n_kv * p.own_parts;
-            const int64_t v = u - p.prefix_units;
+            const int parts = p.n_kv * p.parts, v = u - p.prefix_units;
             int lo = 0, hi = p.B;
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
-                if (static_cast<int64_t>(own_base[mid]) * parts <= v) lo = mid;
+                if (own_base[mid] * parts <= v) lo = mid;
                 else hi = mid;
             }
-            const int tiles = own_base[lo + 1] - own_base[lo];
-            const int64_t rest = v - static_cast<int64_t>(own_base[lo]) * parts;
-            const int part = static_cast<int>(rest / tiles);
+            const int seg = own_base[lo + 1] - own_base[lo], part = (v - own_base[lo] * parts) / seg;
+            u0 = p.prefix_units + own_base[lo] * parts + part * seg;
+            w = ST_LIGHT;
+            tiles = (seg - ST_SEGMENT) / ST_LIGHT;
             f.prefix = f.heavy = false;
-            f.h = part / p.own_parts;
-            f.row0 = part % p.own_parts * ST_ROWS;
-            f.rows = min(ST_ROWS, p.group - f.row0);
+            f.h = part / p.parts;
+            f.c0 = lo * p.parts + (part - f.h * p.parts);
+            f.rows = p.chunk_rows;
+            f.rows2 = 0;
             f.b = lo;
-            f.t0 = rest - static_cast<int64_t>(part) * tiles;
-            f.t1 = min(static_cast<int64_t>(tiles), f.t0 + (end - u));
             f.place = static_cast<int64_t>(cta) + static_cast<int64_t>(lo) * parts + part;
-            u += f.t1 - f.t0;
-            return true;
         }
+        const int stop = min(end, u0 + st_units(tiles, w));
+        f.t0 = st_tiles(u - u0, w);
+        f.t1 = st_tiles(stop - u0, w);
+        u = stop;
+        return true;
     }
     return false;
 }
@@ -175,6 +204,7 @@ __device__ __forceinline__ uint32_t st_pack_bf16x2(float lo, float hi) {
 
 template <int DQK, int DV>
 __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
+                                                                    const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_q_own,
                                                                     const __grid_constant__ StParams p) {
     using C = StShape<DQK, DV>;
     constexpr int KT = C::KT, SLOTS = C::SLOTS;
@@ -188,37 +218,38 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
     if (threadIdx.x == 0) {
         for (int i = 0; i < SLOTS; ++i) { mbar_init(smem_u32(&sh->full[i]), 1); mbar_init(smem_u32(&sh->empty[i]), 1); }
         for (int i = 0; i < ST_INFO; ++i) mbar_init(smem_u32(&sh->info_full[i]), 1);
-        for (int w = 0; w < 2; ++w) { mbar_init(smem_u32(&sh->s_full[w]), 1); mbar_init(smem_u32(&sh->p_full[w]), 4); mbar_init(smem_u32(&sh->o_done[w]), 1); }
-        mbar_init(smem_u32(&sh->q_full), ST_SOFTMAX_WARPS);
-        mbar_init(smem_u32(&sh->left), ST_SOFTMAX_WARPS);
-        mbar_init(smem_u32(&sh->drain), 1);
+        for (int w = 0; w < 2; ++w) { mbar_init(smem_u32(&sh->s_full[w]), 1); mbar_init(smem_u32(&sh->s_free[w]), 4); mbar_init(smem_u32(&sh->p_full[w]), 4); mbar_init(smem_u32(&sh->pv_done[w]), 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&sh->q_full[i]), 1); mbar_init(smem_u32(&sh->q_empty[i]), 1); mbar_init(smem_u32(&sh->meet[i]), 4); mbar_init(smem_u32(&sh->drain[i]), 1); }
+        for (int i = 0; i < ST_FRAGMENTS; ++i) { mbar_init(smem_u32(&sh->f_full[i]), 1); mbar_init(smem_u32(&sh->f_empty[i]), ST_READERS); }
+        mbar_init(smem_u32(&sh->pv_all), 1);
         fence_mbar_init();
         prefetch_tensormap(&tmap_k);
         prefetch_tensormap(&tmap_v);
+        prefetch_tensormap(&tmap_q_own);
     }
     grid_wait();
-    // tiles of every session's own tokens
+    // units of every session's own tokens, per part of its heads
     const int per = (p.B + ST_THREADS - 1) / ST_THREADS, b0 = min(static_cast<int>(threadIdx.x) * per, p.B), b1 = min(b0 + per, p.B);
     int mine = 0;
     for (int b = b0; b < b1; ++b) {
         bool bad;
         const int64_t len = st_length(p, b, bad);
-        const int tiles = len > p.prefix ? static_cast<int>((len - p.own_start + KT - 1) / KT) : 0;
-        sh->own_base[b] = tiles;
-        mine += tiles;
+        const int n = len > p.prefix ? st_units(static_cast<int>((len - p.own_start + KT - 1) / KT), ST_LIGHT) : 0;
+        sh->own_base[b] = n;
+        mine += n;
         if (bad && blockIdx.x == 0) report(p.dev_status, JANUS_DEV_INDEX_OUT_OF_RANGE);
     }
-    int own_tiles;
-    int at = block_exclusive_scan<ST_THREADS>(mine, sh->warp_sums, &own_tiles);
+    int own_units;
+    int at = block_exclusive_scan<ST_THREADS>(mine, sh->warp_sums, &own_units);
     for (int b = b0; b < b1; ++b) {
-        const int tiles = sh->own_base[b];
+        const int n = sh->own_base[b];
         sh->own_base[b] = at;
         if (blockIdx.x == 0) p.own_base[b] = at;
-        at += tiles;
+        at += n;
     }
     if (threadIdx.x == 0) {
-        sh->own_base[p.B] = own_tiles;
-        if (blockIdx.x == 0) p.own_base[p.B] = own_tiles;
+        sh->own_base[p.B] = own_units;
+        if (blockIdx.x == 0) p.own_base[p.B] = own_units;
         // misaligned shared memory, or an earlier CTA that gave up on a wait
         uint32_t flag = (smem_u32(smem) & 1023u) != 0u ? 1u : 0u;
         if (flag != 0u) report(p.dev_status, JANUS_DEV_WAIT_TIMEOUT);
@@ -226,270 +257,406 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
         sh->abort = flag;
     }
     __syncwarp();
-    if (warp == ST_MMA_WARP) { tmem_alloc(smem_u32(&sh->tmem_base), 512); tmem_relinquish(); }
+    if (warp == ST_QK_WARP) { tmem_alloc(smem_u32(&sh->tmem_base), 512); tmem_relinquish(); }
     tc_fence_before();
     __syncthreads();
+    grid_launch_next();      // (tensor memory is allocated)
     tc_fence_after();
     const uint32_t tmem = sh->tmem_base;
-    const int64_t units = p.prefix_units + static_cast<int64_t>(own_tiles) * p.n_kv * p.own_parts;
-    const int cta = blockIdx.x;
-    int64_t u = units * cta / p.n_ctas;
-    const int64_t end = units * (cta + 1) / p.n_ctas;
+    const int units = p.prefix_units + own_units * p.n_kv * p.parts, share = st_share(p, units), cta = blockIdx.x;
+    int u = min(static_cast<int64_t>(share) * cta, static_cast<int64_t>(units));
+    const int end = min(static_cast<int64_t>(u) + share, static_cast<int64_t>(units));
     auto wait_warp = [](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(smem_u32(bar), parity)) != 0; };
     bool ok = true;
     StFragment f;
+    uint32_t n_fragment = 0u;
+    // The next fragment, as the query warp has worked it out.
+    auto next_fragment = [&]() {
+        const uint32_t i = n_fragment % ST_FRAGMENTS;
+        ok = wait_warp(&sh->f_full[i], (n_fragment / ST_FRAGMENTS) & 1u);
+        if (!ok) return false;
+        f = sh->fragment[i];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sh->f_empty[i]));
+        ++n_fragment;
+        return f.last == 0;
+    };
 
-    if (sh->abort != 0u) {
+    const bool start = sh->abort == 0u;
+    // registers: 256 x 208 + 128 x 88 = 384 x 168, what the block was launched with; a raise waits until so many have been given up
+    auto more_registers = [] { asm volatile("setmaxnreg.inc.sync.aligned.u32 208;"); };
+    auto fewer_registers = [] { asm volatile("setmaxnreg.dec.sync.aligned.u32 88;"); };
+    if (!start) {
         // nothing to do
-    } else if (warp == ST_COPY_WARP) {
+    } else if (warp >= ST_SOFTMAX_WARPS) {
+    fewer_registers();      // all four warps: the softmax warps wait for what they give up
+    if (warp == ST_COPY_WARP) {
         // ================================================================== copies
-        // Lane l sees to boxes l, l + 32, ... of a tile.  The pages of a tile are looked up while the one before is copied.
+        // Lane l sees to boxes l, l + 32, ... of a tile.  The pages of the next tile, be it of the next fragment, are looked up between the copies of
+        // K and of V.
         constexpr int MOST = KT / 32;                       // boxes of a lane: a box of one key at least
         const int boxes = KT / p.box;
         uint32_t unit = 0u, tc = 0u;
-        while (ok && st_next(p, sh->own_base, cta, u, end, f)) {
-            int64_t len = p.prefix, base = 0, entries = 0;
-            const int32_t* table = p.prefix_table;
-            if (f.prefix) {
-                entries = (p.prefix + p.page_size - 1) / p.page_size;
-            } else {
-                bool bad;
-                len = st_length(p, f.b, bad);
-                base = p.own_start;
-                const int64_t t = ld_input(p.table_offsets + f.b);
-                entries = t < 0 ? 0 : ld_input(p.table_offsets + f.b + 1) - t;
-                table = p.page_tables + (t < 0 ? 0 : t);
+        int64_t len = 0, base = 0, entries = 0;             // of the fragment of the tile that was looked up last
+        const int32_t* table = nullptr;
+        int t = 0;
+        bool more = true;
+        int id[MOST], row[MOST];
+        bool wanted[MOST];                                  // some key of the box lies in the segment
+        f.t1 = 0;
+        auto look_up = [&]() {                              // the tile after the last one
+            if (++t >= f.t1) {
+                do {
+                    more = next_fragment();
+                    if (!more) return;
+                } while (f.t0 >= f.t1);
+                t = f.t0;
+                if (f.prefix) {
+                    len = p.prefix;
+                    base = 0;
+                    entries = (p.prefix + p.page_size - 1) / p.page_size;
+                    table = p.prefix_table;
+                } else {
+                    bool bad;
+                    const int64_t from = ld_input(p.table_offsets + f.b), to = ld_input(p.table_offsets + f.b + 1);
+                    len = st_length(p, f.b, bad);
+                    base = p.own_start;
+                    entries = from < 0 ? 0 : to - from;
+                    table = p.page_tables + (from < 0 ? 0 : from);
+                }
             }
-            int id[MOST], row[MOST];
-            bool wanted[MOST];                               // some key of the box lies in the segment
-            auto look_up = [&](int64_t t) {
 #pragma unroll
-                for (int j = 0; j < MOST; ++j) {
-                    const int i = lane + 32 * j;
-                    const int64_t pos = base + t * KT + static_cast<int64_t>(i) * p.box;
-                    id[j] = -1;
-                    row[j] = 0;
-                    wanted[j] = i < boxes && t < f.t1 && pos < len && (f.prefix || pos + p.box > p.prefix);
-                    if (wanted[j]) {
-                        const uint32_t x = static_cast<uint32_t>(pos), e = p.page_shift >= 0 ? x >> p.page_shift : x / static_cast<uint32_t>(p.page_size);
-                        row[j] = static_cast<int>(x - e * static_cast<uint32_t>(p.page_size));
-                        if (static_cast<int64_t>(e) < entries) id[j] = ld_input(table + e);
+            for (int j = 0; j < MOST; ++j) {
+                const int i = lane + 32 * j;
+                const int64_t pos = base + static_cast<int64_t>(t) * KT + static_cast<int64_t>(i) * p.box;
+                id[j] = -1;
+                row[j] = 0;
+                wanted[j] = i < boxes && pos < len && (f.prefix || pos + p.box > p.prefix);
+                if (wanted[j]) {
+                    const uint32_t x = static_cast<uint32_t>(pos), e = p.page_shift >= 0 ? x >> p.page_shift : x / static_cast<uint32_t>(p.page_size);
+                    row[j] = static_cast<int>(x - e * static_cast<uint32_t>(p.page_size));
+                    if (static_cast<int64_t>(e) < entries) id[j] = ld_input(table + e);
+                }
+            }
+        };
+        look_up();
+        for (; more && ok; ++tc) {
+            int page[MOST], page_row[MOST];                 // of this tile's boxes; a page past the last where there is nothing to read
+            bool missing = false;
+            const int head = f.h;
+            const int64_t p0 = base + static_cast<int64_t>(t) * KT;
+            const int lo = !f.prefix && p.prefix > p0 ? static_cast<int>(p.prefix - p0) : 0, hi = len - p0 < KT ? static_cast<int>(len - p0) : KT;
+            uint32_t words[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int j = 0; j < MOST; ++j) {
+                const int i = lane + 32 * j;
+                const bool there = wanted[j] && id[j] >= 0 && id[j] < p.n_phys;
+                missing |= wanted[j] && !there;
+                page[j] = there ? id[j] : p.n_phys;
+                page_row[j] = row[j];
+                if (there)
+#pragma unroll
+                    for (int w = 0; w < KT / 32; ++w) {
+                        const int from = max(max(i * p.box, lo) - 32 * w, 0), to = min(min((i + 1) * p.box, hi) - 32 * w, 32);
+                        if (from < to) words[w] |= (to - from == 32 ? 0xffffffffu : ((1u << (to - from)) - 1u) << from);
                     }
-                }
-            };
-            look_up(f.t0);
-            for (int64_t t = f.t0; t < f.t1 && ok; ++t, ++tc) {
-                int page[MOST], page_row[MOST];              // of this tile's boxes; a page past the last where there is nothing to read
-                bool missing = false;
-                const int64_t p0 = base + t * KT;
-                const int lo = !f.prefix && p.prefix > p0 ? static_cast<int>(p.prefix - p0) : 0, hi = len - p0 < KT ? static_cast<int>(len - p0) : KT;
-                uint32_t words[4] = {0u, 0u, 0u, 0u};
+            }
+            bool whole = true;
+#pragma unroll
+            for (int w = 0; w < KT / 32; ++w) {
+                words[w] = __reduce_or_sync(0xffffffffu, words[w]);
+                whole = whole && words[w] == 0xffffffffu;
+            }
+            if (missing) report(p.dev_status, JANUS_DEV_INDEX_OUT_OF_RANGE);
+            if (lane == 0) {
+                const uint32_t n = tc % ST_INFO;
+                sh->partial[n] = whole ? 0u : 1u;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) sh->mask[n][w] = words[w];
+                mbar_arrive(smem_u32(&sh->info_full[n]));
+            }
+            __syncwarp();
+#pragma unroll
+            for (int kv = 0; kv < 2 && ok; ++kv) {
+                const uint32_t slot = unit % SLOTS;
+                ok = wait_warp(&sh->empty[slot], ((unit / SLOTS) & 1u) ^ 1u);
+                if (!ok) break;
+                const uint32_t dst = smem_u32(ring) + slot * C::SLOT, bar = smem_u32(&sh->full[slot]);
+                if (lane == 0) mbar_expect_tx(bar, kv == 0 ? C::K_BYTES : C::V_BYTES);
+                __syncwarp();
 #pragma unroll
                 for (int j = 0; j < MOST; ++j) {
                     const int i = lane + 32 * j;
-                    const bool there = wanted[j] && id[j] >= 0 && id[j] < p.n_phys;
-                    missing |= wanted[j] && !there;
-                    page[j] = there ? id[j] : p.n_phys;
-                    page_row[j] = row[j];
-                    if (there)
+                    if (i >= boxes) continue;
 #pragma unroll
-                        for (int w = 0; w < 4; ++w) {
-                            const int from = max(max(i * p.box, lo) - 32 * w, 0), to = min(min((i + 1) * p.box, hi) - 32 * w, 32);
-                            if (from < to) words[w] |= (to - from == 32 ? 0xffffffffu : ((1u << (to - from)) - 1u) << from);
-                        }
-                }
-                bool whole = true;
-#pragma unroll
-                for (int w = 0; w < KT / 32; ++w) {
-                    words[w] = __reduce_or_sync(0xffffffffu, words[w]);
-                    whole = whole && words[w] == 0xffffffffu;
-                }
-                if (missing) report(p.dev_status, JANUS_DEV_INDEX_OUT_OF_RANGE);
-                if (lane == 0) {
-                    const uint32_t n = tc % ST_INFO;
-                    sh->partial[n] = whole ? 0u : 1u;
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) sh->mask[n][w] = words[w];
+                    for (int a = 0; a < (kv == 0 ? C::QA : C::VA); ++a)
+                        tma_load_4d(dst + a * KT * 128 + i * p.box * 128, kv == 0 ? &tmap_k : &tmap_v, a * 64, page_row[j], head, page[j], bar);
                 }
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&sh->info_full[tc % ST_INFO]));
-                look_up(t + 1);
-#pragma unroll
-                for (int kv = 0; kv < 2 && ok; ++kv, ++unit) {
-                    const uint32_t slot = unit % SLOTS;
-                    ok = wait_warp(&sh->empty[slot], ((unit / SLOTS) & 1u) ^ 1u);
-                    if (!ok) break;
-                    const uint32_t dst = smem_u32(ring) + slot * C::SLOT, bar = smem_u32(&sh->full[slot]);
-                    if (lane == 0) mbar_expect_tx(bar, kv == 0 ? C::K_BYTES : C::V_BYTES);
-                    __syncwarp();
-#pragma unroll
-                    for (int j = 0; j < MOST; ++j) {
-                        const int i = lane + 32 * j;
-                        if (i >= boxes) continue;
-#pragma unroll
-                        for (int a = 0; a < (kv == 0 ? C::QA : C::VA); ++a)
-                            tma_load_4d(dst + a * KT * 128 + i * p.box * 128, kv == 0 ? &tmap_k : &tmap_v, a * 64, page_row[j], f.h, page[j], bar);
-                    }
-                    __syncwarp();
-                }
+                ++unit;
+                if (kv == 0) look_up();
             }
         }
         // Nothing may be on its way into shared memory when the CTA leaves, also after a wait somewhere gave up.
         for (uint32_t n = unit > SLOTS ? unit - SLOTS : 0u; n < unit; ++n)
             if (!wait_warp(&sh->full[n % SLOTS], (n / SLOTS) & 1u)) break;
-    } else if (warp == ST_MMA_WARP) {
-        // ================================================================== MMA issue
-        constexpr uint32_t idesc_qk = umma_idesc_major(1u, ST_ROWS, KT, 0u, 0u), idesc_pv = umma_idesc_major(1u, ST_ROWS, DV, 0u, 1u);
-        const uint32_t q_lo = umma_desc_lo(smem_u32(q_smem), 16), k_lo = umma_desc_lo(smem_u32(ring), 16), v_lo = umma_desc_lo(smem_u32(ring), KT * 128);
-        uint32_t tc = 0u, n_frag = 0u, n_p[2] = {0u, 0u};
-        while (ok && st_next(p, sh->own_base, cta, u, end, f)) {
-            const int64_t tiles = f.t1 - f.t0, steps = f.heavy ? 2 * tiles : tiles;
-            ok = wait_warp(&sh->q_full, n_frag & 1u);
-            if (!ok) break;
-            tc_fence_after();
-            // logits of step n: the group n & 1, tile n or n / 2
-            auto logits = [&](int64_t n) {
+    } else if (warp == ST_QK_WARP) {
+        // ================================================================== MMA issue: logits
+        // Two warps issue MMAs, one Q . K and one P . V: a wait costs a warp some 270 cycles, ready or not, and one warp for both was the bound (3500
+        // cycles for a tile of 256 rows).  What they need of one another goes by barriers.
+        constexpr uint32_t idesc = umma_idesc_major(1u, ST_ROWS, KT, 0u, 0u);
+        const uint32_t q_lo = umma_desc_lo(smem_u32(q_smem), 16), k_lo = umma_desc_lo(smem_u32(ring), 16);
+        uint32_t tc = 0u, n_q = 0u, n_frag = 0u, n_other[2] = {0u, 0u};       // n_other: phases of s_free (more than 128 rows) and ...
+        uint32_t n_pv[2] = {0u, 0u};                                          // ... of pv_done (fewer), by group
+        while (ok && next_fragment()) {
+            const int tiles = f.t1 - f.t0, steps = f.heavy ? 2 * tiles : tiles;
+            if (tiles == 0) continue;
+            // tensor memory is laid out anew: P . V of the fragment before is done
+            ok = n_frag == 0u || wait_warp(&sh->pv_all, (n_frag - 1u) & 1u);
+            ++n_frag;
+            for (int n = 0; n < steps && ok; ++n) {       // step n: group n & 1, tile n or n / 2
                 const uint32_t w = static_cast<uint32_t>(n & 1), un = 2 * (tc + static_cast<uint32_t>(f.heavy ? n >> 1 : n)), slot = un % SLOTS;
-                if (!f.heavy || w == 0u) {
-                    ok = wait_warp(&sh->full[slot], (un / SLOTS) & 1u);
-                    if (!ok) return;
-                    tc_fence_after();
-                }
-                if (elect_one()) {
-                    const uint32_t a = q_lo + (f.heavy ? w * (C::QA * ST_ROWS * 128 >> 4) : 0u), b = k_lo + slot * (C::SLOT >> 4);
-#pragma unroll
-                    for (int i = 0; i < DQK / 16; ++i)
-                        umma_bf16_ss(tmem + w * 128u, a + (i >> 2) * (ST_ROWS * 128 >> 4) + (i & 3) * 2, b + (i >> 2) * (KT * 128 >> 4) + (i & 3) * 2, idesc_qk, i > 0 ? 1u : 0u);
-                    if (!f.heavy || w == 1u) umma_commit(smem_u32(&sh->empty[slot]));
-                    umma_commit(smem_u32(&sh->s_full[w]));
-                }
-                __syncwarp();
-            };
-            logits(0);
-            if (ok && steps > 1) logits(1);
-            for (int64_t n = 0; n < steps && ok; ++n) {
-                const uint32_t w = static_cast<uint32_t>(n & 1), un = 2 * (tc + static_cast<uint32_t>(f.heavy ? n >> 1 : n)) + 1, slot = un % SLOTS;
-                ok = wait_warp(&sh->p_full[w], n_p[w] & 1u);
+                const uint32_t use = n_q + (f.heavy ? w : 0u);
+                if (n == 0 || (f.heavy && n == 1)) ok = wait_warp(&sh->q_full[use & 1u], (use >> 1) & 1u);
                 if (ok && (!f.heavy || w == 0u)) ok = wait_warp(&sh->full[slot], (un / SLOTS) & 1u);
+                if (ok && f.heavy && n > 0) ok = wait_warp(&sh->s_free[w ^ 1u], n_other[w ^ 1u]++ & 1u);      // the other group has the logits before
+                if (ok && !f.heavy && n > 1) ok = wait_warp(&sh->pv_done[w], n_pv[w] & 1u);                   // its P lies where the logits go
+                if (!f.heavy ? n > 1 : false) ++n_pv[w];
                 if (!ok) break;
-                ++n_p[w];
                 tc_fence_after();
                 if (elect_one()) {
-                    const uint32_t b = v_lo + slot * (C::SLOT >> 4);
+                    const uint32_t a = q_lo + (use & 1u) * (C::QA * ST_ROWS * 128 >> 4), b = k_lo + slot * (C::SLOT >> 4), d = tmem + st_col_s(f.heavy, w);
 #pragma unroll
-                    for (int i = 0; i < KT / 16; ++i)
-                        umma_bf16_ts(tmem + ST_COL_O + w * 128u, tmem + w * 128u + 8 * i, b + i * (2048 >> 4), idesc_pv, n > 1 || i > 0 ? 1u : 0u);
+                    for (int i = 0; i < DQK / 16; ++i)
+                        umma_bf16_ss(d, a + (i >> 2) * (ST_ROWS * 128 >> 4) + (i & 3) * 2, b + (i >> 2) * (KT * 128 >> 4) + (i & 3) * 2, idesc, i > 0 ? 1u : 0u);
                     if (!f.heavy || w == 1u) umma_commit(smem_u32(&sh->empty[slot]));
-                    if (n + 2 >= steps) umma_commit(smem_u32(&sh->o_done[w]));
+                    umma_commit(smem_u32(&sh->s_full[w]));
+                    if (f.heavy ? n + 2 >= steps : n + 1 == steps) umma_commit(smem_u32(&sh->q_empty[use & 1u]));
                 }
                 __syncwarp();
-                if (n + 2 < steps) logits(n + 2);
+            }
+            // phases that no logits wait for: those of the last steps
+            if (f.heavy) {
+                if (ok) ok = wait_warp(&sh->s_free[1], n_other[1]++ & 1u);
+                n_pv[0] += static_cast<uint32_t>(tiles);
+                n_pv[1] += static_cast<uint32_t>(tiles);
+            } else {
+                n_pv[0] += 1u;
+                n_pv[1] += steps > 1 ? 1u : 0u;
             }
             tc += static_cast<uint32_t>(tiles);
-            ++n_frag;
+            n_q += f.heavy ? 2u : 1u;
         }
         if (!ok) {                                    // what was issued must be through before tensor memory is given back
-            if (elect_one()) umma_commit(smem_u32(&sh->drain));
+            if (elect_one()) umma_commit(smem_u32(&sh->drain[0]));
             __syncwarp();
-            (void)wait_warp(&sh->drain, 0u);
+            (void)wait_warp(&sh->drain[0], 0u);
         }
+    } else if (warp == ST_PV_WARP) {
+        // ================================================================== MMA issue: outputs
+        constexpr uint32_t idesc = umma_idesc_major(1u, ST_ROWS, DV, 0u, 1u);
+        const uint32_t v_lo = umma_desc_lo(smem_u32(ring), KT * 128);
+        uint32_t tc = 0u, n_p[2] = {0u, 0u};
+        while (ok && next_fragment()) {
+            const int tiles = f.t1 - f.t0, steps = f.heavy ? 2 * tiles : tiles;
+            const bool two = st_copies(f.heavy, f.rows, C::COPIES) > 1;
+            for (int n = 0; n < steps && ok; ++n) {
+                const uint32_t w = static_cast<uint32_t>(n & 1), un = 2 * (tc + static_cast<uint32_t>(f.heavy ? n >> 1 : n)) + 1, slot = un % SLOTS;
+                if (!f.heavy || w == 0u) ok = wait_warp(&sh->full[slot], (un / SLOTS) & 1u);
+                ok = ok && wait_warp(&sh->p_full[w], n_p[w]++ & 1u);
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint32_t b = v_lo + slot * (C::SLOT >> 4), a = tmem + st_col_p(f.heavy, w), d = tmem + ST_COL_O + w * 128u;
+#pragma unroll
+                    for (int i = 0; i < KT / 16; ++i) umma_bf16_ts(d, a + 8 * i, b + i * (2048 >> 4), idesc, n > 1 || i > 0 ? 1u : 0u);
+                    if (two)
+#pragma unroll
+                        for (int i = 0; i < KT / 16; ++i) umma_bf16_ts(d, a + KT / 2 + 8 * i, b + i * (2048 >> 4), idesc, 1u);
+                    if (!f.heavy || w == 1u) umma_commit(smem_u32(&sh->empty[slot]));
+                    umma_commit(smem_u32(&sh->pv_done[w]));
+                    if (n + 1 == steps) umma_commit(smem_u32(&sh->pv_all));
+                }
+                __syncwarp();
+            }
+            tc += static_cast<uint32_t>(tiles);
+        }
+        if (!ok) {
+            if (elect_one()) umma_commit(smem_u32(&sh->drain[1]));
+            __syncwarp();
+            (void)wait_warp(&sh->drain[1], 0u);
+        }
+    } else if (warp == ST_QUERY_WARP) {
+        // ================================================================== fragments, and their queries, ahead of the other warps
+        // Two places of 128 rows: a fragment of more rows takes both, others take them in turn.  Rows that a chunk or a segment does not have hold
+        // whatever comes; nothing is read of what becomes of them.
+        uint32_t n_q = 0u;
+        auto publish = [&]() {
+            const bool more = st_next(p, sh->own_base, cta, u, end, f);
+            const uint32_t i = n_fragment % ST_FRAGMENTS;
+            ok = wait_warp(&sh->f_empty[i], ((n_fragment / ST_FRAGMENTS) & 1u) ^ 1u);
+            if (!ok) return false;
+            ++n_fragment;
+            f.last = more ? 0 : 1;
+            if (lane == 0) {
+                sh->fragment[i] = f;
+                mbar_arrive(smem_u32(&sh->f_full[i]));
+            }
+            __syncwarp();
+            return more;
+        };
+        while (ok && publish()) {
+            if (f.t0 >= f.t1) continue;
+            const int copies = st_copies(f.heavy, f.rows, C::COPIES);
+            for (int w = 0; w < (f.heavy ? 2 : 1) && ok; ++w, ++n_q) {
+                ok = wait_warp(&sh->q_empty[n_q & 1u], ((n_q >> 1) & 1u) ^ 1u);
+                if (!ok) break;
+                const uint32_t dst = smem_u32(q_smem) + (n_q & 1u) * C::Q_PLACE, bar = smem_u32(&sh->q_full[n_q & 1u]);
+                const int c = f.c0 + w * p.per_tile, b = c / p.parts, y = f.h * p.group + (c - b * p.parts) * ST_ROWS;
+                if (f.prefix && copies == 1) {                // one box of 128 rows, as far as whole chunks go
+                    if (elect_one()) {
+                        mbar_expect_tx(bar, static_cast<uint32_t>(C::QA * 128 * p.chunk_rows * p.per_tile));
+#pragma unroll
+                        for (int a = 0; a < C::QA; ++a) tma_load_3d(dst + a * (ST_ROWS * 128), &tmap_q, a * 64, y, b, bar);
+                    }
+                } else {                                      // chunk by chunk, every copy
+                    const int chunks = f.rows / p.chunk_rows;
+                    if (lane == 0) mbar_expect_tx(bar, static_cast<uint32_t>(C::QA * 128 * f.rows * copies));
+                    __syncwarp();
+                    for (int i = lane; i < chunks * copies; i += 32) {
+                        const int copy = i / chunks, j = i - copy * chunks;
+#pragma unroll
+                        for (int a = 0; a < C::QA; ++a)
+                            tma_load_3d(dst + a * (ST_ROWS * 128) + (copy * (ST_ROWS / copies) + j * p.chunk_rows) * 128, &tmap_q_own, a * 64, y, b + j, bar);
+                    }
+                }
+                __syncwarp();
+            }
+        }
+        // (what is on its way has landed before the CTA leaves, also after a wait somewhere gave up)
+        for (uint32_t n = n_q > 2u ? n_q - 2u : 0u; n < n_q; ++n)
+            if (!wait_warp(&sh->q_full[n & 1u], (n >> 1) & 1u)) break;
+    }
     } else {
         // ================================================================== softmax, output
+        more_registers();
         const uint32_t w = static_cast<uint32_t>(warp) >> 2;              // group
         const int r = threadIdx.x & 127;                                  // row of the group, lane of tensor memory
-        const uint32_t lane_addr = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16), s_col = lane_addr + w * 128u, o_col = lane_addr + ST_COL_O + w * 128u;
-        uint32_t tc = 0u, n_s = 0u, n_o = 0u, n_frag = 0u;
-        while (ok && st_next(p, sh->own_base, cta, u, end, f)) {
-            const int64_t tiles = f.t1 - f.t0;
-            const int rows = f.heavy ? min(max(f.rows - static_cast<int>(w) * ST_ROWS, 0), ST_ROWS) : f.rows;      // of this group
-            // ---- queries: those of 128 rows by this group (by the first group where both have the same)
-            if (f.heavy || w == 0u) {
-                constexpr int CH = DQK / 8;                               // 16-byte chunks of a row
-                for (int c = r; c < rows * CH; c += ST_ROWS) {
-                    const int row = c / CH, col = c % CH;
-                    int64_t src;
-                    if (f.prefix) {
-                        const int x = f.row0 + static_cast<int>(w) * ST_ROWS + row, b = x / p.group;
-                        src = static_cast<int64_t>(b) * p.H_q + f.h * p.group + (x - b * p.group);
-                    } else {
-                        src = static_cast<int64_t>(f.b) * p.H_q + f.h * p.group + f.row0 + row;
-                    }
-                    const uint4 v = __ldcg(reinterpret_cast<const uint4*>(p.q + src * DQK) + col);
-                    *reinterpret_cast<uint4*>(q_smem + (w * C::QA + (col >> 3)) * (ST_ROWS * 128) + row * 128 + (((col & 7) ^ (row & 7)) << 4)) = v;
-                }
-                fence_proxy_async();
-            }
-            tc_fence_before();
+        const uint32_t lane_addr = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16), o_col = lane_addr + ST_COL_O + w * 128u;
+        uint32_t tc = 0u, n_s = 0u, n_pv = 0u, n_meet = 0u;
+        auto meet = [&]() {
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&sh->q_full));
-
-            const int64_t first = f.heavy ? 0 : w, step = f.heavy ? 1 : 2;
-            const bool busy = (warp & 3) * 32 < rows;                     // some row of this warp counts
-            float m_ref = neg_inf, l_sum = 0.f;                           // reference maximum (scaled, log2) and sum of this row
-            for (int64_t t = first; t < tiles; t += step) {
+            if (lane == 0) mbar_arrive(smem_u32(&sh->meet[w]));
+            return wait_warp(&sh->meet[w], n_meet++ & 1u);
+        };
+        while (ok && next_fragment()) {
+            const int tiles = f.t1 - f.t0, first = f.heavy ? 0 : static_cast<int>(w), step = f.heavy ? 1 : 2;
+            const int rows = f.heavy && w == 1u ? f.rows2 : f.rows;                // of this group
+            const int copies = st_copies(f.heavy, f.rows, C::COPIES), apart = ST_ROWS / copies, copy = r / apart, row = r - copy * apart;
+            const bool busy = ((warp & 3) * 32) % apart < rows;           // some row of this warp counts
+            const uint32_t s_col = lane_addr + st_col_s(f.heavy, w), p_col = lane_addr + st_col_p(f.heavy, w);
+            float m_ref = neg_inf, l_sum = 0.f;                           // reference maximum (scaled, log2) and sum of this lane
+            // One tile.  N: lanes that share a row's keys; this one has KT / N of them.  With more than one, P goes as two terms, 16 bits of it (the matrix
+            // units wait for memory where rows are few); the first is cut off a little below p, so that both are above zero wherever p is, and an infinite value
+            // stays what it is.
+            auto softmax = [&](auto copies_, bool first_tile, uint32_t info) {
+                constexpr int N = decltype(copies_)::value, KEYS = KT / N, CHUNKS = KEYS / 32, COLS = KEYS / 2;
+                constexpr bool TWO = N > 1;
+                uint32_t x[CHUNKS][32];
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c) tmem_ld32_issue(s_col + copy * KEYS + 32 * c, x[c]);
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c) tmem_ld_wait(x[c]);
+                if (f.heavy) {      // the logits are in registers: the other group's may be computed
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&sh->s_free[w]));
+                }
+                if (sh->partial[info] != 0u) {
+#pragma unroll
+                    for (int c = 0; c < CHUNKS; ++c) {
+                        const uint32_t bits = sh->mask[info][copy * CHUNKS + c];
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) x[c][j] = (bits >> j) & 1u ? x[c][j] : 0xff800000u;
+                    }
+                }
+                float mx[4] = {neg_inf, neg_inf, neg_inf, neg_inf};
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) mx[j & 3] = fmax3(mx[j & 3], __uint_as_float(x[c][2 * j]), __uint_as_float(x[c][2 * j + 1]));
+                const float tile_max = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2e;
+                float corr = 1.f;
+                bool moved = false;
+                if (tile_max > m_ref + 8.f) {
+                    moved = m_ref != neg_inf;
+                    corr = moved ? st_exp2(m_ref - tile_max) : 1.f;
+                    l_sum *= corr;
+                    m_ref = tile_max;
+                }
+                const float neg_m = m_ref == neg_inf ? 0.f : -m_ref;
+                const float2 sc2 = make_float2(p.scale_log2e, p.scale_log2e), nm2 = make_float2(neg_m, neg_m);
+                float2 sum[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                constexpr int ST = COLS < 32 ? COLS : 32;                 // columns of a store
+#pragma unroll
+                for (int c = 0; c < COLS / ST; ++c) {
+                    uint32_t pk[ST], rest[TWO ? ST : 16];
+#pragma unroll
+                    for (int j = 0; j < ST; ++j) {
+                        const int k = 2 * (c * ST + j);
+                        const float2 e = ffma2(make_float2(__uint_as_float(x[k >> 5][k & 31]), __uint_as_float(x[k >> 5][(k & 31) + 1])), sc2, nm2);
+                        const float2 pr = make_float2(st_exp2(e.x), st_exp2(e.y));
+                        if constexpr (TWO) {
+                            const uint32_t lo = __float_as_uint(pr.x * 0.998f), hi = __float_as_uint(pr.y * 0.998f);
+                            pk[j] = __byte_perm(lo, hi, 0x7632);
+                            rest[j] = st_pack_bf16x2(pr.x - __uint_as_float(lo & 0xffff0000u), pr.y - __uint_as_float(hi & 0xffff0000u));
+                        } else {
+                            pk[j] = st_pack_bf16x2(pr.x, pr.y);
+                        }
+                        sum[j & 3] = fadd2(sum[j & 3], pr);
+                    }
+                    if (c == 0) {
+                        // the group's last P . V is done: its P may be overwritten, and O is at rest
+                        if (!first_tile) ok = wait_warp(&sh->pv_done[w], n_pv++ & 1u);
+                        if (!ok) return;
+                        tc_fence_after();
+                        if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll 1
+                            for (int d = 0; d < DV / 32; ++d) {
+                                uint32_t o[32];
+                                tmem_ld32_wait(o_col + 32 * d, o);
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * corr);
+                                tmem_st32_wait(o_col + 32 * d, o);
+                            }
+                        }
+                    }
+                    tmem_st_issue(p_col + copy * COLS + ST * c, pk);
+                    if constexpr (TWO) tmem_st_issue(p_col + KT / 2 + copy * COLS + ST * c, rest);
+                }
+                if constexpr (N > 1) {
+                    // The keys of the other copies do not count for this lane: 2^-126 of each, as 0 would make NaN of an infinite value.
+                    uint32_t zero[COLS];
+#pragma unroll
+                    for (int j = 0; j < COLS; ++j) zero[j] = 0x00800080u;
+#pragma unroll
+                    for (int i = 1; i < N; ++i) {
+                        tmem_st_issue(p_col + ((copy + i) & (N - 1)) * COLS, zero);
+                        if constexpr (TWO) tmem_st_issue(p_col + KT / 2 + ((copy + i) & (N - 1)) * COLS, zero);
+                    }
+                }
+                tmem_st_wait();
+                const float2 s4 = fadd2(fadd2(sum[0], sum[1]), fadd2(sum[2], sum[3]));
+                l_sum += s4.x + s4.y;
+            };
+            for (int t = first; t < tiles; t += step) {
                 const uint32_t tile = tc + static_cast<uint32_t>(t), n = tile % ST_INFO;
                 // (the mask was left before the copies of the tile began: the second wait only makes it visible here)
                 ok = wait_warp(&sh->s_full[w], n_s & 1u) && wait_warp(&sh->info_full[n], (tile / ST_INFO) & 1u);
                 if (!ok) break;
                 ++n_s;
                 tc_fence_after();
-                const bool partial = sh->partial[n] != 0u;
-                if (busy) {
-                    uint32_t x[KT / 32][32];
-#pragma unroll
-                    for (int c = 0; c < KT / 32; ++c) tmem_ld32_issue(s_col + 32 * c, x[c]);
-#pragma unroll
-                    for (int c = 0; c < KT / 32; ++c) tmem_ld_wait(x[c]);
-                    if (partial) {
-#pragma unroll
-                        for (int c = 0; c < KT / 32; ++c) {
-                            const uint32_t bits = sh->mask[n][c];
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) x[c][j] = (bits >> j) & 1u ? x[c][j] : 0xff800000u;
-                        }
-                    }
-                    float mx[4] = {neg_inf, neg_inf, neg_inf, neg_inf};
-#pragma unroll
-                    for (int j = 0; j < KT; j += 2) mx[(j >> 1) & 3] = fmax3(mx[(j >> 1) & 3], __uint_as_float(x[j >> 5][j & 31]), __uint_as_float(x[j >> 5][(j & 31) + 1]));
-                    const float tile_max = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2e;
-                    float corr = 1.f;
-                    bool moved = false;
-                    if (tile_max > m_ref + 8.f) {
-                        moved = m_ref != neg_inf;
-                        corr = moved ? st_exp2(m_ref - tile_max) : 1.f;
-                        l_sum *= corr;
-                        m_ref = tile_max;
-                    }
-                    // O is at rest: s_full stands for all MMAs issued before it, the last P . V of this group among them
-                    if (__any_sync(0xffffffffu, moved)) {
-#pragma unroll 1
-                        for (int c = 0; c < DV / 32; ++c) {
-                            uint32_t o[32];
-                            tmem_ld32_wait(o_col + 32 * c, o);
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * corr);
-                            tmem_st32_wait(o_col + 32 * c, o);
-                        }
-                    }
-                    const float neg_m = m_ref == neg_inf ? 0.f : -m_ref;
-                    const float2 sc2 = make_float2(p.scale_log2e, p.scale_log2e), nm2 = make_float2(neg_m, neg_m);
-                    float2 sum[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-#pragma unroll
-                    for (int c = 0; c < KT / 64; ++c) {
-                        uint32_t pk[32];
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            const float2 e = ffma2(make_float2(__uint_as_float(x[2 * c + (j >> 4)][2 * j & 31]), __uint_as_float(x[2 * c + (j >> 4)][(2 * j & 31) + 1])), sc2, nm2);
-                            const float2 pr = make_float2(st_exp2(e.x), st_exp2(e.y));
-                            pk[j] = st_pack_bf16x2(pr.x, pr.y);
-                            sum[j & 3] = fadd2(sum[j & 3], pr);
-                        }
-                        tmem_st32_wait(s_col + 32 * c, pk);
-                    }
-                    const float2 s4 = fadd2(fadd2(sum[0], sum[1]), fadd2(sum[2], sum[3]));
-                    l_sum += s4.x + s4.y;
-                }
-                if (partial) {
+                if (sh->partial[n] != 0u) {
                     // rows of V that do not count: zeros, once they have landed
                     const uint32_t un = 2 * tile + 1, slot = un % SLOTS;
                     ok = wait_warp(&sh->full[slot], (un / SLOTS) & 1u);
@@ -499,6 +666,14 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
                         for (int c = 0; c < C::VA * 8; ++c) *reinterpret_cast<uint4*>(ring + slot * C::SLOT + (c >> 3) * KT * 128 + r * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
                     fence_proxy_async();
                 }
+                if (busy) {
+                    if (copies == 1) softmax(std::integral_constant<int, 1>{}, t == first, n);
+                    else softmax(std::integral_constant<int, C::COPIES>{}, t == first, n);
+                } else {
+                    if (f.heavy && lane == 0) mbar_arrive(smem_u32(&sh->s_free[w]));
+                    if (t != first) ok = wait_warp(&sh->pv_done[w], n_pv++ & 1u);
+                }
+                if (!ok) break;
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&sh->p_full[w]));
@@ -507,181 +682,234 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
             // ---- what this fragment leaves
             const bool some = first < tiles;
             if (some) {
-                ok = wait_warp(&sh->o_done[w], n_o & 1u);
+                ok = wait_warp(&sh->pv_done[w], n_pv++ & 1u);
                 if (!ok) break;
-                ++n_o;
                 tc_fence_after();
             }
-            const int64_t place = f.prefix ? f.place * 2 * ST_ROWS + w * ST_ROWS + r : (f.place * 2 + w) * p.own_rows + r;
-            if (some && busy) {
-                float4* dst = reinterpret_cast<float4*>((f.prefix ? p.pre_o : p.own_o) + place * DV);
+            // (of a prefix fragment both groups have 128 rows: their own, or outputs of the same rows; of an own one each has chunk_rows)
+            const int pitch = f.prefix ? ST_ROWS : p.chunk_rows;
+            const int64_t place = f.place * 2 + w;
+            float4* dst = reinterpret_cast<float4*>(f.prefix ? p.pre_o : p.own_o) + place * (DV / 4) * pitch;
+            float2* dst_ml = (f.prefix ? p.pre_ml : p.own_ml) + place * pitch;
+            if (!some) {
+                if (r < rows) dst_ml[r] = make_float2(neg_inf, 0.f);
+            } else if (copies == 1) {
+                if (busy)
 #pragma unroll 1
-                for (int c = 0; c < DV / 32; ++c) {
-                    uint32_t o[32];
-                    tmem_ld32_wait(o_col + 32 * c, o);
-                    if (r < rows)
+                    for (int c = 0; c < DV / 32; ++c) {
+                        uint32_t o[32];
+                        tmem_ld32_wait(o_col + 32 * c, o);
+                        if (r < rows)
 #pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            dst[8 * c + j] = make_float4(__uint_as_float(o[4 * j]), __uint_as_float(o[4 * j + 1]), __uint_as_float(o[4 * j + 2]), __uint_as_float(o[4 * j + 3]));
+                            for (int j = 0; j < 8; ++j)
+                                dst[(8 * c + j) * pitch + r] = make_float4(__uint_as_float(o[4 * j]), __uint_as_float(o[4 * j + 1]), __uint_as_float(o[4 * j + 2]), __uint_as_float(o[4 * j + 3]));
+                    }
+                if (r < rows) dst_ml[r] = make_float2(m_ref, l_sum);
+            } else {
+                // the copies of a row become one, through shared memory, in a fixed order
+                const int lanes = copies * rows, dims = lanes <= 32 ? 64 : lanes <= 64 ? 32 : 16, gap = dims + 4;
+                float* join = sh->join[w];
+                sh->ml[w][r] = make_float2(m_ref, l_sum);
+#pragma unroll 1
+                for (int d0 = 0; d0 < DV && ok; d0 += dims) {
+                    if (d0 > 0) ok = meet();                               // what was there has been added up
+                    if (!ok) break;
+#pragma unroll 1
+                    for (int k = 0; k < dims; k += 16) {
+                        uint32_t o[16];
+                        if (busy) tmem_ld16_wait(o_col + d0 + k, o);
+                        if (row < rows)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) *reinterpret_cast<uint4*>(join + (copy * rows + row) * gap + k + 4 * j) = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+                    }
+                    ok = meet();
+                    if (!ok) break;
+                    for (int e = r; e < dims / 4 * rows; e += ST_ROWS) {   // (four dims, row)
+                        const int c4 = e / rows, rr = e - c4 * rows;
+                        float m = neg_inf, l = 0.f;
+                        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                        for (int i = 0; i < C::COPIES; ++i) m = fmaxf(m, sh->ml[w][i * (ST_ROWS / C::COPIES) + rr].x);
+                        const float safe = m == neg_inf ? 0.f : m;
+#pragma unroll
+                        for (int i = 0; i < C::COPIES; ++i) {
+                            const float2 v = sh->ml[w][i * (ST_ROWS / C::COPIES) + rr];
+                            const float4 x = *reinterpret_cast<const float4*>(join + (i * rows + rr) * gap + 4 * c4);
+                            const float g = st_exp2(v.x - safe);
+                            l = fmaf(g, v.y, l);
+                            sum.x = fmaf(g, x.x, sum.x); sum.y = fmaf(g, x.y, sum.y); sum.z = fmaf(g, x.z, sum.z); sum.w = fmaf(g, x.w, sum.w);
+                        }
+                        dst[(d0 / 4 + c4) * pitch + rr] = sum;
+                        if (d0 == 0 && c4 == 0) dst_ml[rr] = make_float2(m, l);
+                    }
                 }
+                ok = ok && meet();                                         // (before the next fragment's)
+                if (!ok) break;
             }
-            if (r < rows) (f.prefix ? p.pre_ml : p.own_ml)[place] = make_float2(m_ref, l_sum);
             tc += static_cast<uint32_t>(tiles);
-            // a group without a tile in a fragment would run ahead and arrive on q_full for two fragments before the other has for one
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&sh->left));
-            ok = wait_warp(&sh->left, n_frag++ & 1u);
         }
     }
     if (!ok && lane == 0) report(p.dev_status, JANUS_DEV_WAIT_TIMEOUT);
     tc_fence_before();
     __syncthreads();
-    if (warp == ST_MMA_WARP) {
+    if (warp == ST_QK_WARP) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
 }
 
-// ---- merge: a block per row, its warps take the row's fragments in turn
-constexpr int SM_WARPS = 4;
+// ---- merge: a block takes eight rows that lie one behind the other in the segments (128 bytes of every output at a time); its threads are
+// (row, four dims, share of the row's outputs), HERE fours of dims.  32 outputs of a row at a time: a warp works out their weights, then all threads add them up.
+constexpr int SM_ROWS = 8;
 
-template <int DV>
-__global__ void __launch_bounds__(32 * SM_WARPS) attn_shared_merge_kernel(const __grid_constant__ StParams p) {
-    constexpr int PER = DV / 32;
+// A row's outputs in a segment: one from every fragment (more than 128 rows), or one from each group of every fragment.
+struct SmPart {
+    int n, row, step;
+    int64_t place;                       // of the first, in groups; step to the next
+};
+
+template <int DV, int HERE, int SHARES>
+__global__ void __launch_bounds__(SM_ROWS * HERE * SHARES) attn_shared_merge_kernel(const __grid_constant__ StParams p) {
+    constexpr int CHUNKS = DV / 4;
     grid_launch_next();
-    grid_wait();
-    __shared__ float acc_s[SM_WARPS][DV];
-    __shared__ float red[SM_WARPS], l_s[SM_WARPS];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t row = blockIdx.x;
-    const int b = static_cast<int>(row / p.H_q), hq = static_cast<int>(row - static_cast<int64_t>(b) * p.H_q), h = hq / p.group, g = hq - h * p.group;
+    __shared__ SmPart parts_s[SM_ROWS][2];
+    __shared__ float weight[SM_ROWS][32], scale_s[SM_ROWS], sum_s[SM_ROWS], max_s[SM_ROWS];
+    __shared__ float4 acc_s[SHARES > 1 ? SHARES - 1 : 1][HERE][SM_ROWS];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const float neg_inf = __int_as_float(0xff800000);
-    bool bad;
-    const int64_t len = st_length(p, b, bad);
-    const int base0 = ld_input(p.own_base + b), base1 = ld_input(p.own_base + b + 1), all = ld_input(p.own_base + p.B);
-    const int parts = p.n_kv * p.own_parts;
-    const int64_t units = p.prefix_units + static_cast<int64_t>(all) * parts;
-    // CTA whose stretch holds unit x
-    auto cta_of = [&](int64_t x) {
-        int64_t i = x * p.n_ctas / units;
-        while (i + 1 < p.n_ctas && units * (i + 1) / p.n_ctas <= x) ++i;
-        while (i > 0 && units * i / p.n_ctas > x) --i;
-        return static_cast<int>(i);
-    };
-    // fragments of the prefix segment, then of the own one: the first CTA of each, how many, and groups with an output of this row
-    int pre_cta = 0, n_pre = 0, pre_groups = 1, own_cta = 0, n_own = 0, seg = 0, pre_row = 0;
-    int64_t own_seg = 0, seg_u0 = 0;
-    int seg_w = 1;
-    if (len > 0 && p.prefix > 0) {
-        const int x = b * p.group + g;
-        seg = x / (2 * ST_ROWS) * p.n_kv + h;
-        pre_row = x % (2 * ST_ROWS);
-        st_prefix_segment(p, seg, seg_u0, seg_w);
-        pre_groups = seg_w == ST_HEAVY_UNITS ? 1 : 2;
-        pre_cta = cta_of(seg_u0);
-        n_pre = cta_of(seg_u0 + seg_w * p.prefix_tiles - 1) - pre_cta + 1;
-    }
-    if (base1 > base0) {
-        const int part = h * p.own_parts + g / ST_ROWS;
-        own_seg = static_cast<int64_t>(b) * parts + part;
-        const int64_t u0 = p.prefix_units + static_cast<int64_t>(base0) * parts + static_cast<int64_t>(part) * (base1 - base0);
-        own_cta = cta_of(u0);
-        n_own = cta_of(u0 + (base1 - base0) - 1) - own_cta + 1;
-    }
-    const int n_a = n_pre * pre_groups, n = n_a + 2 * n_own;
-    // maximum and sum of output i of the row (-inf, 0: none), and where it lies
-    auto fragment = [&](int i, const float*& o) {
-        if (i < n_a) {
-            const int f = i / pre_groups, w = i - f * pre_groups, cta = pre_cta + f;
-            int64_t from = units * cta / p.n_ctas, to = units * (cta + 1) / p.n_ctas;
-            from = from > seg_u0 ? from : seg_u0;
-            to = to < seg_u0 + seg_w * p.prefix_tiles ? to : seg_u0 + seg_w * p.prefix_tiles;
-            if (st_tile(from, seg_u0, seg_w) >= st_tile(to, seg_u0, seg_w)) return make_float2(neg_inf, 0.f);      // no tile begins in its stretch
-            const int64_t place = (static_cast<int64_t>(cta) + seg) * 2 * ST_ROWS + w * ST_ROWS + pre_row;
-            o = p.pre_o + place * DV;
-            return __ldcg(p.pre_ml + place);
+    grid_wait();
+    const int x_rows = p.B * p.group, blocks = (x_rows + SM_ROWS - 1) / SM_ROWS, h = blockIdx.x / blocks, x0 = (blockIdx.x - h * blocks) * SM_ROWS;
+    // a lane for each row's segment in the prefix, one for its own
+    if (tid < 2 * SM_ROWS) {
+        SmPart part = {};
+        const int x = x0 + (tid >> 1), b = x / p.group, g = x - b * p.group;
+        bool bad;
+        if (x < x_rows && st_length(p, b, bad) > 0) {
+            const int segments = p.n_kv * p.parts, share = st_share(p, p.prefix_units + ld_input(p.own_base + p.B) * segments), sub = g / ST_ROWS, c = b * p.parts + sub;
+            if ((tid & 1) == 0 && p.prefix > 0) {
+                const int tile = c / (2 * p.per_tile), in_tile = c - tile * 2 * p.per_tile, half = in_tile >= p.per_tile ? 1 : 0, s = tile * p.n_kv + h;
+                int w;
+                const int u0 = st_prefix_segment(p, s, w), cta = u0 / share;
+                part.n = (u0 + st_units(p.prefix_tiles, w) - 1) / share - cta + 1;
+                part.place = 2 * (static_cast<int64_t>(cta) + s) + half;
+                part.step = 2;
+                if (s >= p.heavy_segments) { part.n *= 2; part.step = 1; }
+                part.row = (in_tile - half * p.per_tile) * p.chunk_rows + (g - sub * ST_ROWS);
+            }
+            if ((tid & 1) != 0) {
+                const int base = ld_input(p.own_base + b), seg = ld_input(p.own_base + b + 1) - base;
+                if (seg > 0) {
+                    const int k = h * p.parts + sub, u0 = p.prefix_units + base * segments + k * seg, cta = u0 / share;
+                    part.n = 2 * ((u0 + seg - 1) / share - cta + 1);
+                    part.place = 2 * (static_cast<int64_t>(cta) + static_cast<int64_t>(b) * segments + k);
+                    part.step = 1;
+                    part.row = g - sub * ST_ROWS;
+                }
+            }
         }
-        const int f = (i - n_a) >> 1, w = (i - n_a) & 1, cta = own_cta + f;
-        if (units * cta / p.n_ctas == units * (cta + 1) / p.n_ctas) return make_float2(neg_inf, 0.f);               // more CTAs than tiles
-        const int64_t place = ((cta + own_seg) * 2 + w) * p.own_rows + g % ST_ROWS;
-        o = p.own_o + place * DV;
-        return __ldcg(p.own_ml + place);
-    };
-    float m = neg_inf;
-    const float* o = nullptr;
-    for (int i = threadIdx.x; i < n; i += 32 * SM_WARPS) m = fmaxf(m, fragment(i, o).x);
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    if (lane == 0) red[warp] = m;
-    __syncthreads();
-    m = red[0];
-#pragma unroll
-    for (int i = 1; i < SM_WARPS; ++i) m = fmaxf(m, red[i]);
-    const float safe = m == neg_inf ? 0.f : m;
-    float acc[PER] = {}, l = 0.f;
-#pragma unroll 4
-    for (int i = warp; i < n; i += SM_WARPS) {
-        const float2 ml = fragment(i, o);
-        if (ml.x == neg_inf && ml.y == 0.f) continue;      // nothing there (a sum that is not a number counts)
-        const float f = st_exp2(ml.x - safe);
-        l = fmaf(f, ml.y, l);
-        if constexpr (PER == 4) {
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(o) + lane);
-            acc[0] = fmaf(f, v.x, acc[0]); acc[1] = fmaf(f, v.y, acc[1]); acc[2] = fmaf(f, v.z, acc[2]); acc[3] = fmaf(f, v.w, acc[3]);
-        } else {
-            const float2 v = __ldcg(reinterpret_cast<const float2*>(o) + lane);
-            acc[0] = fmaf(f, v.x, acc[0]); acc[1] = fmaf(f, v.y, acc[1]);
-        }
+        parts_s[tid >> 1][tid & 1] = part;
     }
-#pragma unroll
-    for (int e = 0; e < PER; ++e) acc_s[warp][lane * PER + e] = acc[e];
-    if (lane == 0) l_s[warp] = l;
     __syncthreads();
-    if (warp == 0) {
-        l = 0.f;
+    const int row = tid % SM_ROWS, here = tid / SM_ROWS % HERE, chunk = blockIdx.y * HERE + here, share = tid / (SM_ROWS * HERE);
+    int most = 0;
 #pragma unroll
-        for (int i = 0; i < SM_WARPS; ++i) l += l_s[i];
+    for (int r = 0; r < SM_ROWS; ++r) most = max(most, parts_s[r][0].n + parts_s[r][1].n);
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float m = neg_inf, l = 0.f;          // of row `warp`: maximum so far, this lane's part of the sum
+    const bool weighs = warp < SM_ROWS;
+    const SmPart pre_w = parts_s[warp % SM_ROWS][0], own_w = parts_s[warp % SM_ROWS][1], pre = parts_s[row][0], own = parts_s[row][1];
+    auto left = [&](int i) {             // maximum and sum of output i of row `warp`
+        if (i < pre_w.n) return __ldcg(p.pre_ml + (pre_w.place + pre_w.step * i) * ST_ROWS + pre_w.row);
+        if (i < pre_w.n + own_w.n) return __ldcg(p.own_ml + (own_w.place + (i - pre_w.n)) * p.chunk_rows + own_w.row);
+        return make_float2(neg_inf, 0.f);
+    };
+    float2 next = make_float2(neg_inf, 0.f);
+    if (weighs) next = left(lane);
+    const float4* const pre_o = reinterpret_cast<const float4*>(p.pre_o) + (pre.place * CHUNKS + chunk) * ST_ROWS + pre.row;
+    const float4* const own_o = reinterpret_cast<const float4*>(p.own_o) + (own.place * CHUNKS + chunk) * p.chunk_rows + own.row;
+    const int64_t pre_step = static_cast<int64_t>(pre.step) * CHUNKS * ST_ROWS, own_step = static_cast<int64_t>(CHUNKS) * p.chunk_rows;
+    for (int i0 = 0; i0 < most; i0 += 32) {
+        if (weighs) {
+            const float2 v = next;
+            next = left(i0 + 32 + lane);
+            float top = fmaxf(m, v.x);
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            const float safe = top == neg_inf ? 0.f : top, old = st_exp2(m - safe), f = st_exp2(v.x - safe);
+            const bool empty = v.x == neg_inf && v.y == 0.f;      // (a sum that is not a number counts)
+            l = l * old + (empty ? 0.f : f * v.y);
+            m = top;
+            weight[warp][lane] = empty ? -1.f : f;
+            if (lane == 0) scale_s[warp] = old;
+        }
+        __syncthreads();
+        if (i0 > 0) {
+            const float f0 = scale_s[row];
+            acc.x *= f0; acc.y *= f0; acc.z *= f0; acc.w *= f0;
+        }
+        const int count = min(32, pre.n + own.n - i0);
+#pragma unroll 8
+        for (int j = share; j < count; j += SHARES) {
+            const float f1 = weight[row][j];
+            const int i = i0 + j;
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (f1 >= 0.f || f1 != f1) o = __ldcg(i < pre.n ? pre_o + i * pre_step : own_o + (i - pre.n) * own_step);
+            acc.x = fmaf(f1, o.x, acc.x); acc.y = fmaf(f1, o.y, acc.y); acc.z = fmaf(f1, o.z, acc.z); acc.w = fmaf(f1, o.w, acc.w);
+        }
+        __syncthreads();
+    }
+    if (weighs) {
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+        if (lane == 0) { sum_s[warp] = l; max_s[warp] = m; }
+    }
+    if (SHARES > 1 && share > 0) acc_s[share - 1][here][row] = acc;
+    __syncthreads();
+    const int x = x0 + row;
+    if (share == 0 && x < x_rows) {
+#pragma unroll
+        for (int i = 0; i < SHARES - 1; ++i) {
+            const float4 v = acc_s[i][here][row];
+            acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
+        }
+        l = sum_s[row];
+        m = max_s[row];
         const float inv = l != 0.f ? 1.f / l : 0.f;        // (a NaN is a sum)
-        uint32_t wd[PER / 2];
-#pragma unroll
-        for (int e = 0; e < PER; e += 2) {
-            float x = 0.f, y = 0.f;
-#pragma unroll
-            for (int i = 0; i < SM_WARPS; ++i) { x += acc_s[i][lane * PER + e]; y += acc_s[i][lane * PER + e + 1]; }
-            wd[e / 2] = st_pack_bf16x2(x * inv, y * inv);
-        }
-        if constexpr (PER == 4) *reinterpret_cast<uint2*>(p.out + row * DV + lane * PER) = make_uint2(wd[0], wd[1]);
-        else *reinterpret_cast<uint32_t*>(p.out + row * DV + lane * PER) = wd[0];
-        if (p.lse != nullptr && lane == 0) p.lse[row] = l != 0.f ? (safe + log2f(l)) * 0.6931471805599453f : neg_inf;
+        const int b = x / p.group;
+        const int64_t out = static_cast<int64_t>(b) * p.H_q + h * p.group + (x - b * p.group);
+        *reinterpret_cast<uint2*>(p.out + out * DV + 4 * chunk) = make_uint2(st_pack_bf16x2(acc.x * inv, acc.y * inv), st_pack_bf16x2(acc.z * inv, acc.w * inv));
+        if (p.lse != nullptr && chunk == 0) p.lse[out] = l != 0.f ? ((m == neg_inf ? 0.f : m) + log2f(l)) * 0.6931471805599453f : neg_inf;
     }
 }
 
 // ---- host
 bool attn_shared_tc_supported(int d_qk, int d_v) { return (d_qk == 64 || d_qk == 128 || d_qk == 192) && (d_v == 64 || d_v == 128); }
 
-// Places of the fragments, and what they take of the workspace.
+// Chunks of rows, places of the fragments, and what they take of the workspace.
 struct StLayout {
-    int64_t row_tiles, prefix_segments, pre_places, own_places;
-    int own_rows, own_parts;
+    int chunk_rows, parts, per_tile;
+    int64_t chunks, row_tiles, prefix_segments, pre_places, own_places;
     size_t own_base, pre_ml, own_ml, pre_o, own_o, bytes;      // byte offsets
 };
 
 static StLayout st_layout(int B, int H_q, int n_kv, int d_v, int64_t prefix, int64_t max_len) {
     StLayout l;
     const int group = H_q / n_kv;
-    l.own_rows = group < ST_ROWS ? group : ST_ROWS;
-    l.own_parts = (group + ST_ROWS - 1) / ST_ROWS;
-    l.row_tiles = (static_cast<int64_t>(B) * group + 2 * ST_ROWS - 1) / (2 * ST_ROWS);
+    l.chunk_rows = group < ST_ROWS ? group : ST_ROWS;
+    l.parts = (group + ST_ROWS - 1) / ST_ROWS;
+    l.per_tile = ST_ROWS / l.chunk_rows;
+    l.chunks = static_cast<int64_t>(B) * l.parts;
+    l.row_tiles = (l.chunks + 2 * l.per_tile - 1) / (2 * l.per_tile);
     l.prefix_segments = prefix > 0 ? l.row_tiles * n_kv : 0;
     l.pre_places = prefix > 0 ? l.prefix_segments + ST_MAX_CTAS : 0;
-    l.own_places = max_len > prefix ? static_cast<int64_t>(B) * n_kv * l.own_parts + ST_MAX_CTAS : 0;
+    l.own_places = max_len > prefix ? l.chunks * n_kv + ST_MAX_CTAS : 0;
     size_t at = 0;
     auto take = [&](size_t n) { const size_t x = at; at += (n + 127) & ~static_cast<size_t>(127); return x; };
     l.own_base = take(sizeof(int32_t) * (static_cast<size_t>(B) + 1));
     l.pre_ml = take(sizeof(float2) * l.pre_places * 2 * ST_ROWS);
-    l.own_ml = take(sizeof(float2) * l.own_places * 2 * l.own_rows);
+    l.own_ml = take(sizeof(float2) * l.own_places * 2 * l.chunk_rows);
     l.pre_o = take(sizeof(float) * l.pre_places * 2 * ST_ROWS * d_v);
-    l.own_o = take(sizeof(float) * l.own_places * 2 * l.own_rows * d_v);
+    l.own_o = take(sizeof(float) * l.own_places * 2 * l.chunk_rows * d_v);
     l.bytes = at;
     return l;
 }
@@ -690,21 +918,34 @@ size_t attn_shared_tc_workspace(int B, int H_q, int n_kv, int d_v, int64_t prefi
     return st_layout(B < ST_MAX_SESSIONS ? B : ST_MAX_SESSIONS, H_q, n_kv, d_v, prefix, max_len).bytes;
 }
 
-// Pool [pages, page_size, heads, d] as a 4-D tensor (d, token, head, page); boxes of 64 dims x `box` tokens.
-static bool st_tmap(CUtensorMap* map, const void* base, int d, int page_size, int heads, int64_t pages, int64_t page_stride, int64_t tok_stride, int64_t head_stride, int box) {
+static bool st_encode(CUtensorMap* map, const void* base, int axes, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
     PFN_encodeTiled enc = get_encode_tiled();
     if (enc == nullptr) return false;
-    const cuuint64_t dims[4] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(page_size), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(pages > 0 ? pages : 1)};
-    // (the stride of an axis of one does not matter, but is looked at)
-    const cuuint64_t strides[3] = {static_cast<cuuint64_t>(page_size > 1 ? tok_stride * 2 : 16), static_cast<cuuint64_t>(heads > 1 ? head_stride * 2 : 16),
-                                   static_cast<cuuint64_t>(pages > 1 ? page_stride * 2 : 16)};
-    const cuuint32_t boxes[4] = {64, static_cast<cuuint32_t>(box), 1, 1}, estr[4] = {1, 1, 1, 1};
+    const cuuint32_t estr[4] = {1, 1, 1, 1};
     if (current_context_id() == 0) {      // the encoder is a driver call and wants a context on this thread
         int dev = 0;
         if (cudaGetDevice(&dev) != cudaSuccess || cudaSetDevice(dev) != cudaSuccess) return false;
     }
-    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, boxes, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, axes, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Pool [pages, page_size, heads, d] as a 4-D tensor (d, token, head, page); boxes of 64 dims x `box` tokens.
+static bool st_tmap(CUtensorMap* map, const void* base, int d, int page_size, int heads, int64_t pages, int64_t page_stride, int64_t tok_stride, int64_t head_stride, int box) {
+    const cuuint64_t dims[4] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(page_size), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(pages > 0 ? pages : 1)};
+    // (the stride of an axis of one does not matter, but is looked at)
+    const cuuint64_t strides[3] = {static_cast<cuuint64_t>(page_size > 1 ? tok_stride * 2 : 16), static_cast<cuuint64_t>(heads > 1 ? head_stride * 2 : 16),
+                                   static_cast<cuuint64_t>(pages > 1 ? page_stride * 2 : 16)};
+    const cuuint32_t boxes[4] = {64, static_cast<cuuint32_t>(box), 1, 1};
+    return st_encode(map, base, 4, dims, strides, boxes);
+}
+
+// Queries [sessions, heads, d]; boxes of 64 dims x a chunk x so many sessions.
+static bool st_tmap_q(CUtensorMap* map, const void* base, int d, int heads, int sessions, int chunk_rows, int box_sessions) {
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(sessions)};
+    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(d) * 2, static_cast<cuuint64_t>(d) * 2 * heads};
+    const cuuint32_t boxes[3] = {64, static_cast<cuuint32_t>(chunk_rows), static_cast<cuuint32_t>(box_sessions)};
+    return st_encode(map, base, 3, dims, strides, boxes);
 }
 
 template <int DQK, int DV>
@@ -725,11 +966,18 @@ static int st_launch(const SharedAttnArgs& a, StParams p, cudaStream_t stream) {
         !st_tmap(&map_v, a.v_pool, DV, p.page_size, p.n_kv, p.n_phys, a.v_page_stride, a.v_tok_stride, a.v_head_stride, box))
         return JANUS_ERR_CUDA;
     p.own_start = p.prefix / box * box;
-    p.prefix_tiles = (p.prefix + C::KT - 1) / C::KT;
-    const int64_t own_most = p.max_len > p.prefix ? (p.max_len - p.own_start + C::KT - 1) / C::KT : 0;
-    for (int b = 0; b < a.B; b += ST_MAX_SESSIONS) {
-        p.B = a.B - b < ST_MAX_SESSIONS ? a.B - b : ST_MAX_SESSIONS;
-        if (own_most * p.B > INT32_MAX) return JANUS_ERR_UNSUPPORTED;
+    const int64_t prefix_tiles = (p.prefix + C::KT - 1) / C::KT, own_most = p.max_len > p.prefix ? (p.max_len - p.own_start + C::KT - 1) / C::KT : 0;
+    const int ctas = sms < ST_MAX_CTAS ? sms : ST_MAX_CTAS;
+    // so many sessions at a time that units count in 31 bits, however long the sessions turn out to be
+    constexpr int64_t MOST_UNITS = 1 << 30;
+    const StLayout most_l = st_layout(a.B < ST_MAX_SESSIONS ? a.B : ST_MAX_SESSIONS, p.H_q, p.n_kv, DV, p.prefix, p.max_len);
+    const int64_t own_units = own_most > 0 ? (own_most * ST_LIGHT + ST_SEGMENT) * p.n_kv * most_l.parts : 0;
+    const int64_t prefix_units = (prefix_tiles * ST_HEAVY + ST_SEGMENT) * most_l.prefix_segments;
+    if (own_units > MOST_UNITS || prefix_units > MOST_UNITS) return JANUS_ERR_UNSUPPORTED;
+    int at_once = ST_MAX_SESSIONS;
+    if (own_units > 0 && MOST_UNITS / own_units < at_once) at_once = static_cast<int>(MOST_UNITS / own_units);
+    for (int b = 0; b < a.B; b += at_once) {
+        p.B = a.B - b < at_once ? a.B - b : at_once;
         const StLayout l = st_layout(p.B, p.H_q, p.n_kv, DV, p.prefix, p.max_len);
         unsigned char* ws = static_cast<unsigned char*>(a.ws);
         p.own_base = reinterpret_cast<int32_t*>(ws + l.own_base);
@@ -737,22 +985,26 @@ static int st_launch(const SharedAttnArgs& a, StParams p, cudaStream_t stream) {
         p.own_ml = reinterpret_cast<float2*>(ws + l.own_ml);
         p.pre_o = reinterpret_cast<float*>(ws + l.pre_o);
         p.own_o = reinterpret_cast<float*>(ws + l.own_o);
-        p.own_rows = l.own_rows;
-        p.own_parts = l.own_parts;
-        p.prefix_segments = static_cast<int>(l.prefix_segments);
-        const int64_t last_rows = static_cast<int64_t>(p.B) * p.group - (l.row_tiles - 1) * 2 * ST_ROWS;
-        p.heavy_segments = p.prefix > 0 ? static_cast<int>((l.row_tiles - (last_rows > ST_ROWS ? 0 : 1)) * p.n_kv) : 0;
-        p.prefix_units = (static_cast<int64_t>(p.heavy_segments) * ST_HEAVY_UNITS + (p.prefix_segments - p.heavy_segments)) * p.prefix_tiles;
-        const int64_t most = p.prefix_units + own_most * p.B * p.n_kv * p.own_parts;
-        const int ctas = sms < ST_MAX_CTAS ? sms : ST_MAX_CTAS;
+        p.chunk_rows = l.chunk_rows; p.parts = l.parts; p.per_tile = l.per_tile; p.chunks = static_cast<int>(l.chunks);
+        const int64_t last = l.chunks - (l.row_tiles - 1) * 2 * l.per_tile;
+        p.heavy_segments = p.prefix > 0 ? static_cast<int>((l.row_tiles - (last > l.per_tile ? 0 : 1)) * p.n_kv) : 0;
+        p.prefix_tiles = static_cast<int>(prefix_tiles);
+        p.prefix_units = static_cast<int>(p.heavy_segments * (prefix_tiles * ST_HEAVY + ST_SEGMENT) + (l.prefix_segments - p.heavy_segments) * (prefix_tiles * ST_LIGHT + ST_SEGMENT));
+        const int64_t most = p.prefix_units + own_units * p.B;
         p.n_ctas = static_cast<int>(most < 1 ? 1 : most < ctas ? most : ctas);
         p.q = static_cast<const uint16_t*>(a.q) + static_cast<int64_t>(b) * p.H_q * DQK;
         p.out = static_cast<uint16_t*>(a.out) + static_cast<int64_t>(b) * p.H_q * DV;
         p.lse = a.lse != nullptr ? a.lse + static_cast<int64_t>(b) * p.H_q : nullptr;
         p.kv_lens = a.kv_lens + b;
         p.table_offsets = a.table_offsets != nullptr ? a.table_offsets + b : nullptr;
-        JANUS_CUDA_CHECK(launch_kernel(attn_shared_kernel<DQK, DV>, dim3(p.n_ctas), ST_THREADS, C::SMEM, stream, 1, map_k, map_v, p));
-        JANUS_CUDA_CHECK(launch_kernel(attn_shared_merge_kernel<DV>, dim3(static_cast<unsigned>(p.B) * p.H_q), 32 * SM_WARPS, 0, stream, 1, p));
+        CUtensorMap map_q, map_q_own;
+        if (!st_tmap_q(&map_q, p.q, DQK, p.H_q, p.B, l.chunk_rows, l.per_tile) || !st_tmap_q(&map_q_own, p.q, DQK, p.H_q, p.B, l.chunk_rows, 1)) return JANUS_ERR_CUDA;
+        JANUS_CUDA_CHECK(launch_kernel(attn_shared_kernel<DQK, DV>, dim3(p.n_ctas), ST_THREADS, C::SMEM, stream, 1, map_k, map_v, map_q, map_q_own, p));
+        // Few rows have many outputs each: eight shares of them, and the dims in several blocks (32 rows with 64 outputs each 7.1 us; one block 13.0).
+        // Many rows fill the SMs with a block for eight rows (3072 rows: 7.3 us; dims in several blocks 20.8).
+        const int64_t blocks = (static_cast<int64_t>(p.B) * p.group + SM_ROWS - 1) / SM_ROWS * p.n_kv;
+        if (blocks <= ST_MAX_CTAS) JANUS_CUDA_CHECK(launch_kernel(attn_shared_merge_kernel<DV, 4, 8>, dim3(static_cast<unsigned>(blocks), DV / 16), 256, 0, stream, 1, p));
+        else JANUS_CUDA_CHECK(launch_kernel(attn_shared_merge_kernel<DV, DV / 4, 128 / DV>, dim3(static_cast<unsigned>(blocks)), 256, 0, stream, 1, p));
     }
     return JANUS_OK;
 }
