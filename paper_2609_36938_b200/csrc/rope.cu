@@ -10,15 +10,20 @@
 //
 // What bounds it: HBM; three flops per element.  A thread takes one 16-byte chunk of the head dimension (half layout: two, half the rotated
 // part apart), works out the sines and cosines of its pairs once and applies them to the same chunk of up to RP_HEADS heads of its
-// token, all loads of which are under way together.  Consecutive threads take consecutive chunks, then heads, then tokens.
+// token.  Consecutive threads take consecutive chunks, then heads, then tokens.  Two heads a thread: 4096 tokens x 128 heads, 64 dims of 576: 37.8 us (134 MB of
+// 128-byte pieces, 3.5 TB/s), 777 x 32 x 128 in fp32 4.7 us (5.4 TB/s), rows of 4096 tokens into the cache with 32 query heads 20.1 us; four heads 39.9, 5.1 and
+// 26.8 (fewer warps); one 44.1, 5.6 and 23.2 (angles).  Sines and cosines of a block's tokens in shared memory, each worked out once: 82.9, 10.4
+// and 38.8 (the barrier keeps loads and stores apart).  Loads ahead of the look at the position: 40.2, 5.1 and 21.1 (registers).
 #include <cuda_fp16.h>
+
+#include <algorithm>
 
 #include "janus_common.cuh"
 
 namespace janus {
 
 constexpr int RP_THREADS = 256;
-constexpr int RP_HEADS = 4;
+constexpr int RP_HEADS = 2;
 constexpr int RP_JOBS = 3;           // queries, keys, values
 
 // Rows of one tensor: heads h of rows t from src to dst.  `rot` = 0: copied only.
@@ -32,7 +37,7 @@ struct RpJob {
     int chunks;                      // per head
     int groups;                      // heads g, g + groups, ... are one thread's
     bool rotate, paged;
-    uint32_t first_block;
+    uint32_t first_block, inv_row, inv_chunks;       // 2^32 / (groups * chunks), 2^32 / chunks
 };
 
 struct RpParams {
@@ -50,16 +55,25 @@ struct RpParams {
     int32_t* dev_status;
 };
 
-// sine and cosine of phase * 2^-64 turns
+// Sine and cosine of phase * 2^-64 turns: the nearest quarter turn is taken off, and of what is left, at most an eighth, the Taylor series: the first
+// terms left out, a^11 / 11! and a^12 / 12!, are below 2^-29.
 __device__ __forceinline__ void rp_turn(uint64_t phase, float& s, float& c) {
-    const uint64_t q = (phase + (1ull << 61)) >> 62;                                        // nearest quarter turn
-    const int32_t rest = static_cast<int32_t>(static_cast<int64_t>(phase - (q << 62)) >> 32);   // within an eighth of a turn of it, in 2^-32 turns
-    float s0, c0;
-    sincospif(static_cast<float>(rest) * 4.656612873077393e-10f, &s0, &c0);                 // 2^-31: half turns
+    const uint32_t top = static_cast<uint32_t>(phase >> 32), q = (top + (1u << 29)) >> 30;
+    const float a = static_cast<float>(static_cast<int32_t>(top - (q << 30))) * 1.4629180792671596e-9f, b = a * a;      // 2 pi 2^-32
+    const float s0 = fmaf(a * b, fmaf(b, fmaf(b, fmaf(b, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f), a);
+    const float c0 = fmaf(b, fmaf(b, fmaf(b, fmaf(b, fmaf(b, -1.f / 3628800.f, 1.f / 40320.f), -1.f / 720.f), 1.f / 24.f), -0.5f), 1.f);
     s = (q & 1u) ? c0 : s0;
     c = (q & 1u) ? s0 : c0;
     if (q & 2u) s = -s;
-    if ((q + 1) & 2u) c = -c;
+    if ((q + 1u) & 2u) c = -c;
+}
+
+// u / d with m = 2^32 / d, rounded down: the estimate is at most two short.
+__device__ __forceinline__ uint32_t rp_divide(uint32_t u, uint32_t d, uint32_t m) {
+    uint32_t q = __umulhi(u, m), r = u - q * d;
+    if (r >= d) { ++q; r -= d; }
+    if (r >= d) ++q;
+    return q;
 }
 
 template <class T>
@@ -103,11 +117,11 @@ __global__ void __launch_bounds__(RP_THREADS) rope_kernel(const RpParams p) {
         in_row = static_cast<uint32_t>(unit - static_cast<uint64_t>(t) * per_row);
     } else {
         const uint32_t u = static_cast<uint32_t>(unit);
-        t = u / per_row;
+        t = rp_divide(u, per_row, job.inv_row);
         in_row = u - static_cast<uint32_t>(t) * per_row;
     }
     if (t >= p.T) return;
-    const int g = static_cast<int>(in_row / job.chunks), chunk = static_cast<int>(in_row - g * job.chunks);
+    const int g = static_cast<int>(rp_divide(in_row, job.chunks, job.inv_chunks)), chunk = static_cast<int>(in_row - g * job.chunks);
 
     // which bytes of a head this thread moves, and whether it turns them
     constexpr int CB = VEC * static_cast<int>(sizeof(T)), COPY_VEC = CB == 16 ? VEC : 1, COPY_BYTES = COPY_VEC * static_cast<int>(sizeof(T));
@@ -209,6 +223,8 @@ static int rp_launch(RpParams& p, bool wide, cudaStream_t stream) {
         while (per < RP_HEADS && threads / per > 148 * 2048) per *= 2;
         j.groups = (j.H + per - 1) / per;
         j.first_block = static_cast<uint32_t>(blocks);
+        j.inv_row = static_cast<uint32_t>(std::min<uint64_t>((1ull << 32) / (static_cast<uint64_t>(j.groups) * j.chunks), UINT32_MAX));
+        j.inv_chunks = static_cast<uint32_t>(std::min<uint64_t>((1ull << 32) / j.chunks, UINT32_MAX));
         blocks += (static_cast<uint64_t>(p.T) * j.groups * j.chunks + RP_THREADS - 1) / RP_THREADS;
         if (blocks > 0x7fffffffu) return JANUS_ERR_UNSUPPORTED;
     }
