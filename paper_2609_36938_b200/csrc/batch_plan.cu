@@ -149,23 +149,19 @@ __global__ void __launch_bounds__(BP_THREADS) batch_plan_kernel(const BpParams p
     if (first && over) report(p.dev_status, JANUS_DEV_CAPACITY_EXCEEDED);
     __syncthreads();
 
-    // page j of session b, -1 where there is none
-    auto page_of = [&](int b, int32_t j, bool& fresh) -> int32_t {
+    // page j of session b as it stands in the block table or the free list; INT32_MIN where the free list has ended
+    auto load_page = [&](int b, int32_t j, bool& fresh) -> int32_t {
         const int32_t held = page_sum[b + 1] - page_sum[b] - (free_sum[b + 1] - free_sum[b]);
         fresh = j >= held;
-        int32_t id;
-        if (fresh) {
-            const int64_t rank = static_cast<int64_t>(free_sum[b]) + (j - held);
-            if (rank >= p.n_free) return -1;        // (reported with the counts)
-            id = ld_input(p.free_pages + rank);
-        } else {
-            id = ld_input(p.block_tables + b * p.block_ld + j);
-        }
-        if (id < 0 || id >= p.n_phys) {
-            report(p.dev_status, JANUS_DEV_INDEX_OUT_OF_RANGE);
-            id = -1;
-        }
-        return id;
+        const int64_t rank = static_cast<int64_t>(free_sum[b]) + (j - held);
+        if (fresh && rank >= p.n_free) return INT32_MIN;      // (reported with the counts)
+        return max(fresh ? ld_input(p.free_pages + rank) : ld_input(p.block_tables + b * p.block_ld + j), -1);
+    };
+    // ... and as it goes out: -1 where there is none
+    auto checked = [&](int32_t id) -> int32_t {
+        if (id >= 0 && id < p.n_phys) return id;
+        if (id != INT32_MIN) report(p.dev_status, JANUS_DEV_INDEX_OUT_OF_RANGE);
+        return -1;
     };
 
     const int64_t stride = static_cast<int64_t>(gridDim.x) * BP_THREADS;
@@ -180,7 +176,7 @@ __global__ void __launch_bounds__(BP_THREADS) batch_plan_kernel(const BpParams p
             pos = (c > 0 ? c : 0) + (r - row_sum[b]);
             const int64_t j = p.page_shift >= 0 ? pos >> p.page_shift : pos / p.page_size;
             bool fresh;
-            const int32_t id = j < page_sum[b + 1] - page_sum[b] ? page_of(b, static_cast<int32_t>(j), fresh) : -1;
+            const int32_t id = j < page_sum[b + 1] - page_sum[b] ? checked(load_page(b, static_cast<int32_t>(j), fresh)) : -1;
             if (id >= 0) {
                 slot = static_cast<int64_t>(id) * p.page_size + (pos - j * p.page_size);
                 if (p.key_rows != nullptr) key_row = ld_input(p.key_offsets + b) + pos;
@@ -191,13 +187,32 @@ __global__ void __launch_bounds__(BP_THREADS) batch_plan_kernel(const BpParams p
         p.slots[r] = slot;
         if (p.key_rows != nullptr) p.key_rows[r] = key_row;
     }
-    for (int64_t e = at; e < page_sum[p.B]; e += stride) {
-        const int b = bp_find(page_sum, p.B, e);
-        const int32_t j = static_cast<int32_t>(e - page_sum[b]);
-        bool fresh;
-        const int32_t id = page_of(b, j, fresh);
-        if (fresh) p.block_tables[b * p.block_ld + j] = id;
-        if (e < p.table_capacity) p.page_tables[e] = id;
+    // Where the threads would go round several times, four consecutive entries at a time: one search, and their loads go together (1024 sessions
+    // of up to 131072 tokens 11.9 -> 9.2 us; eight 10.2; twelve sessions 4.7, with four entries a thread 5.4).
+    constexpr int AT_ONCE = 4;
+    const int64_t entries = page_sum[p.B];
+    const int per_turn = entries > stride ? AT_ONCE : 1;
+    for (int64_t e = at * per_turn; e < entries; e += stride * per_turn) {
+        int b = bp_find(page_sum, p.B, e);
+        int32_t id[AT_ONCE], j[AT_ONCE];
+        int session[AT_ONCE];
+        bool fresh[AT_ONCE];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            fresh[k] = false;
+            if (k >= per_turn || e + k >= entries) continue;
+            while (e + k >= page_sum[b + 1]) ++b;
+            session[k] = b;
+            j[k] = static_cast<int32_t>(e + k - page_sum[b]);
+            id[k] = load_page(b, j[k], fresh[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            if (k >= per_turn || e + k >= entries) continue;
+            id[k] = checked(id[k]);
+            if (fresh[k]) p.block_tables[session[k] * p.block_ld + j[k]] = id[k];
+            if (e + k < p.table_capacity) p.page_tables[e + k] = id[k];
+        }
     }
 }
 
