@@ -706,26 +706,38 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
                     }
                 if (r < rows) dst_ml[r] = make_float2(m_ref, l_sum);
             } else {
-                // the copies of a row become one, through shared memory, in a fixed order
+                // The copies of a row become one, through shared memory, in a fixed order: up to eight rows 64 dims at a time, more rows fewer.
                 const int lanes = copies * rows, dims = lanes <= 32 ? 64 : lanes <= 64 ? 32 : 16, gap = dims + 4;
-                float* join = sh->join[w];
+                float* const join = sh->join[w];
+                float* const mine = join + (copy * rows + row) * gap;
                 sh->ml[w][r] = make_float2(m_ref, l_sum);
+                auto leave = [&](const auto& o, int at) {
+#pragma unroll
+                    for (int j = 0; j < static_cast<int>(sizeof(o) / 16); ++j) *reinterpret_cast<uint4*>(mine + at + 4 * j) = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+                };
 #pragma unroll 1
                 for (int d0 = 0; d0 < DV && ok; d0 += dims) {
                     if (d0 > 0) ok = meet();                               // what was there has been added up
                     if (!ok) break;
+                    if (dims == 64) {
+                        uint32_t o[2][32];
+                        tmem_ld32_issue(o_col + d0, o[0]);
+                        tmem_ld32_issue(o_col + d0 + 32, o[1]);
+                        tmem_ld_wait(o[0]);
+                        tmem_ld_wait(o[1]);
+                        if (row < rows) { leave(o[0], 0); leave(o[1], 32); }
+                    } else {
 #pragma unroll 1
-                    for (int k = 0; k < dims; k += 16) {
-                        uint32_t o[16];
-                        if (busy) tmem_ld16_wait(o_col + d0 + k, o);
-                        if (row < rows)
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) *reinterpret_cast<uint4*>(join + (copy * rows + row) * gap + k + 4 * j) = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+                        for (int k = 0; k < dims; k += 16) {
+                            uint32_t o[16];
+                            tmem_ld16_wait(o_col + d0 + k, o);
+                            if (row < rows) leave(o, k);
+                        }
                     }
                     ok = meet();
                     if (!ok) break;
                     for (int e = r; e < dims / 4 * rows; e += ST_ROWS) {   // (four dims, row)
-                        const int c4 = e / rows, rr = e - c4 * rows;
+                        const int rr = e >> (dims == 64 ? 4 : dims == 32 ? 3 : 2), c4 = e & (dims / 4 - 1);
                         float m = neg_inf, l = 0.f;
                         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
