@@ -1,20 +1,29 @@
 // Dense attention of one query token per session over a shared prefix and each session's own tokens: the entry point, and the route by
 // listed tokens.
 //
-// Listed tokens.  The sparse attention kernels take any selection, so also all tokens: a kernel writes for every session one page table (pages
-// of the prefix, then its own) and the list of its tokens.  That is the way of layouts whose work is bound by the matrix units for one session
-// already, so that reading the prefix once for all gains nothing (latent: 128 heads read one row per token, 242 flops a byte), and of head
-// dims without a kernel of their own.
+// Listed tokens.  The sparse attention kernels take any selection, so also all tokens: a kernel writes page tables (pages of the prefix, then the
+// session's own) and lists of tokens.  That is the way of layouts whose work is bound by the matrix units for one session already, so that reading the
+// prefix once for all gains nothing (latent: 128 heads read one row per token, 242 flops a byte), and of head dims without a kernel of their own.
+//
+// For the latent layout a session's keys are cut into pieces of equal length, each a row of the selection with an output of its own, so that every
+// pair of SMs has work whatever the sessions' lengths; the pieces that there are form a compact list, whose length the attention kernel reads from device
+// memory, and a last kernel joins them by their log-sum-exp.
 #include "attn_shared.cuh"
 
 namespace janus {
 
-int sparse_attn_listed(const void* q, int M, int H_q, int d_qk, const void* k_pool, const void* v_pool, int64_t page_stride, int64_t tok_stride,
-                       int64_t head_stride, int64_t v_page_stride, int64_t v_tok_stride, int64_t v_head_stride, int n_kv_heads, int d_v, const int32_t* idx, int k,
-                       int page_size, const int32_t* page_tables, const int64_t* table_offsets, float softmax_scale, void* out, float* lse, int32_t* dev_status,
-                       cudaStream_t stream);
+int launch_sparse_attn_generic(const void* q, int M, int H_q, int d_qk, const void* k_pool, const void* v_pool, int64_t page_stride,
+                               int64_t tok_stride, int64_t head_stride, int64_t v_page_stride, int64_t v_tok_stride, int64_t v_head_stride, int n_kv_heads,
+                               int d_v, const int32_t* idx, int k, int page_size, const int32_t* page_table, int64_t n_logical_pages,
+                               const int64_t* table_offsets, float softmax_scale, void* out, float* lse, int32_t* dev_status, cudaStream_t stream);
+bool sparse_attn_latent_tc_supported(int M, int H_q, int d_qk, const void* k_pool, const void* v_pool, int64_t page_stride,
+                                     int64_t tok_stride, int n_kv_heads, int d_v, int k);
+int launch_latent_pieces(const void* q, int n_tokens, int max_rows, const int32_t* rows, const int32_t* token_of, const void* pool, int64_t page_stride,
+                         int64_t tok_stride, const int32_t* idx, int k, int page_size, const int32_t* page_tables, const int64_t* table_offsets,
+                         float softmax_scale, void* out, float* lse, int32_t* dev_status, cudaStream_t stream);
 
 constexpr int SL_THREADS = 256;
+constexpr int SL_HEADS = 128, SL_DV = 512;      // latent layout
 
 struct SlParams {
     const int32_t* prefix_table;
@@ -23,22 +32,53 @@ struct SlParams {
     const int64_t* kv_lens;
     int64_t prefix, max_len, n_phys;
     int B, page_size, prefix_pages, first_own, width;      // first_own: page of a session's table that holds token `prefix`
-    int k;
-    int32_t* idx;              // [B, k]
-    int32_t* tables;           // [B, width]
-    int64_t* offsets;          // [B + 1]
+    int k, pieces;             // tokens of a row, rows of a session at most
+    int32_t* idx;              // [rows, k]
+    int32_t* tables;           // [rows, width]
+    int64_t* offsets;          // [rows + 1]
+    int32_t* row_base;         // [B + 1]: rows of the sessions before
+    int32_t* token_of;         // [rows]: session of a row
+    bool compact;              // only rows that there are; else `pieces` (one) for every session
     int32_t* dev_status;
 };
 
-// One block per session and stretch of its tokens and pages.
+__device__ __forceinline__ int64_t sl_length(const SlParams& p, int b, bool& bad) {
+    const int64_t len = ld_input(p.kv_lens + b);
+    bad = len > p.max_len || len < 0 || (len > 0 && len < p.prefix);
+    return len > p.max_len ? p.max_len : len < p.prefix ? 0 : len;
+}
+
+// A block per piece of a session.
 __global__ void __launch_bounds__(SL_THREADS) shared_list_kernel(const SlParams p) {
     grid_launch_next();
+    __shared__ int sums[SL_THREADS / 32];
     grid_wait();
-    const int b = blockIdx.y;
-    int64_t len = ld_input(p.kv_lens + b);
-    if (len > p.max_len || len < 0 || (len > 0 && len < p.prefix)) {
-        if (threadIdx.x == 0 && blockIdx.x == 0) report(p.dev_status, JANUS_DEV_INDEX_OUT_OF_RANGE);
-        len = len > p.max_len ? p.max_len : 0;
+    const int b = blockIdx.y, piece = blockIdx.x;
+    bool bad;
+    const int64_t len = sl_length(p, b, bad);
+    if (bad && threadIdx.x == 0 && piece == 0) report(p.dev_status, JANUS_DEV_INDEX_OUT_OF_RANGE);
+    int row = b * p.pieces + piece;
+    if (p.compact) {           // rows of the sessions before this one
+        int before = 0;
+        for (int i = threadIdx.x; i < b; i += SL_THREADS) before += static_cast<int>((sl_length(p, i, bad) + p.k - 1) / p.k);
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) before += __shfl_xor_sync(0xffffffffu, before, d);
+        if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = before;
+        __syncthreads();
+        before = 0;
+#pragma unroll
+        for (int w = 0; w < SL_THREADS / 32; ++w) before += sums[w];
+        const int here = static_cast<int>((len + p.k - 1) / p.k);
+        row = before + piece;
+        if (piece == 0 && threadIdx.x == 0) {
+            p.row_base[b] = before;
+            if (b == p.B - 1) p.row_base[p.B] = before + here;
+        }
+        if (piece >= here) {
+            if (b == p.B - 1 && piece == here && threadIdx.x == 0) p.offsets[row] = static_cast<int64_t>(row) * p.width;
+            return;
+        }
+        if (threadIdx.x == 0) p.token_of[row] = b;
     }
     int64_t table = 0, entries = 0;
     if (p.max_len > p.prefix) {
@@ -48,38 +88,109 @@ __global__ void __launch_bounds__(SL_THREADS) shared_list_kernel(const SlParams 
     }
     // a page of the prefix that also holds a session's first own tokens is there twice: the tokens behind it are one page further on
     const int shift = p.prefix % p.page_size != 0 ? p.page_size : 0;
-    const int64_t n = static_cast<int64_t>(p.k) > p.width ? p.k : p.width;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * SL_THREADS + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * SL_THREADS) {
-        if (i < p.k) p.idx[static_cast<int64_t>(b) * p.k + i] = i < len ? static_cast<int32_t>(i + (i < p.prefix ? 0 : shift)) : -1;
-        if (i < p.width) {
-            int32_t id = -1;
-            if (i < p.prefix_pages) {
-                id = ld_input(p.prefix_table + i);
-            } else {
-                const int64_t j = i - p.prefix_pages + p.first_own;
-                if (j < entries) id = ld_input(p.page_tables + table + j);
-            }
-            p.tables[static_cast<int64_t>(b) * p.width + i] = id < p.n_phys ? id : -1;
+    const int64_t first = static_cast<int64_t>(piece) * p.k;
+    for (int i = threadIdx.x; i < p.k; i += SL_THREADS) {
+        const int64_t s = first + i;
+        p.idx[static_cast<int64_t>(row) * p.k + i] = s < len ? static_cast<int32_t>(s + (s < p.prefix ? 0 : shift)) : -1;
+    }
+    // the pages that the row's tokens lie in (places in its table), by one block of the session all of them where rows are not compact
+    const int64_t last = first + p.k < len ? first + p.k : len;
+    int e0 = 0, e1 = p.width;
+    if (p.compact && last > first) {
+        e0 = static_cast<int>((first + (first < p.prefix ? 0 : shift)) / p.page_size);
+        e1 = static_cast<int>((last - 1 + (last - 1 < p.prefix ? 0 : shift)) / p.page_size) + 1;
+    }
+    for (int i = e0 + threadIdx.x; i < e1; i += SL_THREADS) {
+        int32_t id = -1;
+        if (i < p.prefix_pages) {
+            id = ld_input(p.prefix_table + i);
+        } else {
+            const int64_t j = static_cast<int64_t>(i) - p.prefix_pages + p.first_own;
+            if (j < entries) id = ld_input(p.page_tables + table + j);
+        }
+        p.tables[static_cast<int64_t>(row) * p.width + i] = id < p.n_phys ? id : -1;
+    }
+    if (threadIdx.x == 0) {
+        p.offsets[row] = static_cast<int64_t>(row) * p.width;
+        if (b == p.B - 1 && piece == p.pieces - 1) p.offsets[row + 1] = static_cast<int64_t>(row + 1) * p.width;
+    }
+}
+
+// Output of a session from those of its pieces, and their log-sum-exps: 64 threads per head, eight dims each.
+__global__ void __launch_bounds__(SL_THREADS) shared_join_kernel(const uint16_t* piece_out, const float* piece_lse, const int32_t* row_base, uint16_t* out, float* lse) {
+    grid_launch_next();
+    grid_wait();
+    constexpr float LOG2E = 1.4426950408889634f;
+    const int b = blockIdx.y, h = blockIdx.x * (SL_THREADS / 64) + threadIdx.x / 64, d = threadIdx.x % 64 * 8;
+    const int r0 = ld_input(row_base + b), r1 = ld_input(row_base + b + 1);
+    const float neg_inf = __int_as_float(0xff800000);
+    float m = neg_inf, l = 0.f, acc[8] = {};
+#pragma unroll 8
+    for (int r = r0; r < r1; ++r) m = fmaxf(m, __ldcg(piece_lse + static_cast<int64_t>(r) * SL_HEADS + h));
+    const float safe = m == neg_inf ? 0.f : m;
+#pragma unroll 8
+    for (int r = r0; r < r1; ++r) {
+        const int64_t at = static_cast<int64_t>(r) * SL_HEADS + h;
+        const float v = __ldcg(piece_lse + at), f = exp2f((v - safe) * LOG2E);
+        const uint4 x = __ldcg(reinterpret_cast<const uint4*>(piece_out + at * SL_DV + d));
+        if (v == neg_inf) continue;
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        l += f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            acc[2 * j] = fmaf(f, __uint_as_float(w[j] << 16), acc[2 * j]);
+            acc[2 * j + 1] = fmaf(f, __uint_as_float(w[j] & 0xffff0000u), acc[2 * j + 1]);
         }
     }
-    if (blockIdx.x == 0 && threadIdx.x == 0) {
-        p.offsets[b] = static_cast<int64_t>(b) * p.width;
-        if (b == p.B - 1) p.offsets[p.B] = static_cast<int64_t>(p.B) * p.width;
+    const float inv = l != 0.f ? 1.f / l : 0.f;        // (a NaN is a sum)
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(acc[2 * j] * inv, acc[2 * j + 1] * inv);
+        w[j] = *reinterpret_cast<const uint32_t*>(&v);
     }
+    const int64_t at = static_cast<int64_t>(b) * SL_HEADS + h;
+    *reinterpret_cast<uint4*>(out + at * SL_DV + d) = make_uint4(w[0], w[1], w[2], w[3]);
+    if (lse != nullptr && d == 0) lse[at] = l != 0.f ? safe + logf(l) : neg_inf;
 }
 
-// Sizes of the lists; false where a token's number would pass 31 bits.
-static bool sl_sizes(int page_size, int64_t prefix, int64_t max_len, int64_t* prefix_pages, int64_t* width) {
-    *prefix_pages = (prefix + page_size - 1) / page_size;
-    *width = *prefix_pages + (max_len + page_size - 1) / page_size - prefix / page_size;
-    return max_len <= INT32_MAX - 2 * static_cast<int64_t>(page_size);
-}
+// Lists of the route by listed tokens, and where they lie in the workspace.
+struct SlLayout {
+    int64_t prefix_pages, width, pieces, rows;
+    int k;
+    size_t offsets, row_base, token_of, tables, idx, lse, out, bytes;
+};
 
-static size_t sl_bytes(int B, int page_size, int64_t prefix, int64_t max_len) {
-    int64_t prefix_pages, width;
-    if (!sl_sizes(page_size, prefix, max_len, &prefix_pages, &width)) return 0;
-    auto round = [](size_t n) { return (n + 15) & ~static_cast<size_t>(15); };
-    return round(sizeof(int64_t) * (static_cast<size_t>(B) + 1)) + round(sizeof(int32_t) * static_cast<size_t>(B) * width) + round(sizeof(int32_t) * static_cast<size_t>(B) * max_len);
+static bool sl_latent(int H_q, int d_qk, int n_kv_heads, int d_v) { return H_q == SL_HEADS && d_qk == 576 && n_kv_heads == 1 && d_v == SL_DV; }
+
+static SlLayout sl_layout(int B, bool latent, int page_size, int64_t prefix, int64_t max_len) {
+    SlLayout l = {};
+    l.prefix_pages = (prefix + page_size - 1) / page_size;
+    l.width = l.prefix_pages + (max_len + page_size - 1) / page_size - prefix / page_size;
+    l.k = static_cast<int>(max_len);
+    if (latent) {
+        // A pair of SMs takes 1.5 us for 128 tokens and 0.6 us for a row; the rows go to 74 pairs in turn.  The length with the least time for
+        // sessions of max_len is taken (24 sessions of 9216: 1024, 216 rows).
+        double best = 0.;
+        for (int k = 256; k <= 4096; k *= 2) {
+            const int64_t rows = B * ((max_len + k - 1) / k), turns = (rows + 73) / 74;
+            const double t = turns * (k / 128 * 1.5 + 0.6) + rows * 0.04;      // (and what the join reads)
+            if (k == 256 || t < best) { best = t; l.k = k; }
+        }
+    }
+    l.pieces = latent ? (max_len + l.k - 1) / l.k : 1;
+    l.rows = B * l.pieces;
+    size_t at = 0;
+    auto take = [&](size_t n) { const size_t x = at; at += (n + 127) & ~static_cast<size_t>(127); return x; };
+    l.offsets = take(sizeof(int64_t) * (l.rows + 1));
+    l.row_base = take(latent ? sizeof(int32_t) * (static_cast<size_t>(B) + 1) : 0);
+    l.token_of = take(latent ? sizeof(int32_t) * l.rows : 0);
+    l.tables = take(sizeof(int32_t) * l.rows * l.width);
+    l.idx = take(sizeof(int32_t) * l.rows * l.k);
+    l.lse = take(latent ? sizeof(float) * l.rows * SL_HEADS : 0);
+    l.out = take(latent ? 2ull * l.rows * SL_HEADS * SL_DV : 0);
+    l.bytes = at;
+    return l;
 }
 
 }  // namespace janus
@@ -88,7 +199,7 @@ extern "C" size_t janus_attn_decode_shared_workspace_size(int B, int H_q, int d_
     using namespace janus;
     if (B <= 0 || H_q <= 0 || d_qk <= 0 || n_kv_heads <= 0 || d_v <= 0 || page_size <= 0 || prefix_len < 0 || max_len < prefix_len) return 0;
     if (attn_shared_tc_supported(d_qk, d_v)) return attn_shared_tc_workspace(B, H_q, n_kv_heads, d_v, prefix_len, max_len);
-    return sl_bytes(B, page_size, prefix_len, max_len);
+    return sl_layout(B, sl_latent(H_q, d_qk, n_kv_heads, d_v), page_size, prefix_len, max_len).bytes;
 }
 
 extern "C" int janus_attn_decode_shared(const void* q, int B, int H_q, int d_qk, const void* k_pool, int64_t k_page_stride, int64_t k_tok_stride,
@@ -121,21 +232,35 @@ extern "C" int janus_attn_decode_shared(const void* q, int B, int H_q, int d_qk,
                                       d_v, page_size, n_phys_pages, prefix_table, prefix_len, page_tables, table_offsets, kv_lens, max_len, softmax_scale, out, lse, ws,
                                       dev_status}, stream);
 
+    // (the two kernels of this route: the latent one takes aliased values alone)
+    const bool latent = sl_latent(H_q, d_qk, n_kv_heads, d_v) && max_len > 0 &&
+                        sparse_attn_latent_tc_supported(B, H_q, d_qk, k_pool, v_pool, k_page_stride, k_tok_stride, n_kv_heads, d_v, 256);
+    const SlLayout l = sl_layout(B, latent, page_size, prefix_len, max_len);
+    if (l.rows > (1 << 30) / SL_HEADS || l.pieces > 0x7fffffff || l.width > INT32_MAX) return JANUS_ERR_UNSUPPORTED;
+    unsigned char* base = static_cast<unsigned char*>(ws);
     SlParams p;
     p.prefix_table = prefix_table; p.page_tables = page_tables; p.table_offsets = table_offsets; p.kv_lens = kv_lens;
     p.prefix = prefix_len; p.max_len = max_len; p.n_phys = n_phys_pages;
     p.B = B; p.page_size = page_size;
-    int64_t prefix_pages, width;
-    sl_sizes(page_size, prefix_len, max_len, &prefix_pages, &width);
-    p.prefix_pages = static_cast<int>(prefix_pages); p.first_own = static_cast<int>(prefix_len / page_size); p.width = static_cast<int>(width);
-    p.k = static_cast<int>(max_len);
-    p.offsets = static_cast<int64_t*>(ws);
-    p.tables = reinterpret_cast<int32_t*>(static_cast<unsigned char*>(ws) + ((sizeof(int64_t) * (B + 1) + 15) & ~static_cast<size_t>(15)));
-    p.idx = p.tables + ((static_cast<size_t>(B) * width + 3) & ~static_cast<size_t>(3));
+    p.prefix_pages = static_cast<int>(l.prefix_pages); p.first_own = static_cast<int>(prefix_len / page_size); p.width = static_cast<int>(l.width);
+    p.k = l.k; p.pieces = static_cast<int>(l.pieces);
+    p.offsets = reinterpret_cast<int64_t*>(base + l.offsets);
+    p.row_base = reinterpret_cast<int32_t*>(base + l.row_base);
+    p.token_of = reinterpret_cast<int32_t*>(base + l.token_of);
+    p.tables = reinterpret_cast<int32_t*>(base + l.tables);
+    p.idx = reinterpret_cast<int32_t*>(base + l.idx);
+    p.compact = latent;
     p.dev_status = dev_status;
-    const int64_t most = p.k > p.width ? p.k : p.width, blocks = (most + 4 * SL_THREADS - 1) / (4 * SL_THREADS);
-    const dim3 grid(static_cast<unsigned>(blocks < 1 ? 1 : blocks < 64 ? blocks : 64), static_cast<unsigned>(B));
-    JANUS_CUDA_CHECK(launch_kernel(shared_list_kernel, grid, SL_THREADS, 0, stream, 1, p));
-    return sparse_attn_listed(q, B, H_q, d_qk, k_pool, v_pool, k_page_stride, k_tok_stride, k_head_stride, v_page_stride, v_tok_stride, v_head_stride, n_kv_heads, d_v, p.idx,
-                              p.k, page_size, p.tables, p.offsets, softmax_scale, out, lse, dev_status, stream);
+    JANUS_CUDA_CHECK(launch_kernel(shared_list_kernel, dim3(static_cast<unsigned>(l.pieces), static_cast<unsigned>(B)), SL_THREADS, 0, stream, 1, p));
+    if (!latent)
+        return launch_sparse_attn_generic(q, B, H_q, d_qk, k_pool, v_pool, k_page_stride, k_tok_stride, k_head_stride, v_page_stride, v_tok_stride, v_head_stride,
+                                          n_kv_heads, d_v, p.idx, p.k, page_size, p.tables, 0, p.offsets, softmax_scale, out, lse, dev_status, stream);
+    uint16_t* piece_out = reinterpret_cast<uint16_t*>(base + l.out);
+    float* piece_lse = reinterpret_cast<float*>(base + l.lse);
+    const int rc = launch_latent_pieces(q, B, static_cast<int>(l.rows), p.row_base + B, p.token_of, k_pool, k_page_stride, k_tok_stride, p.idx, p.k, page_size, p.tables,
+                                        p.offsets, softmax_scale, piece_out, piece_lse, dev_status, stream);
+    if (rc != JANUS_OK) return rc;
+    JANUS_CUDA_CHECK(launch_kernel(shared_join_kernel, dim3(SL_HEADS / (SL_THREADS / 64), static_cast<unsigned>(B)), SL_THREADS, 0, stream, 1, piece_out, piece_lse, p.row_base,
+                                   static_cast<uint16_t*>(out), lse));
+    return JANUS_OK;
 }

@@ -73,8 +73,7 @@ struct StShared {
     uint32_t partial[ST_INFO];                      // whether some key of the tile does not count
     uint32_t mask[ST_INFO][4];
     StFragment fragment[ST_FRAGMENTS];
-    uint32_t tmem_base, abort;
-    int warp_sums[33];
+    uint32_t tmem_base;
     float2 ml[2][ST_ROWS];                          // by group: maxima and sums of the copies, to be joined,
     alignas(16) float join[2][ST_ROWS * ST_JOIN];   // and their outputs, some dims at a time
     int32_t own_base[ST_MAX_SESSIONS + 1];          // tiles of the sessions before, per kv head
@@ -136,8 +135,8 @@ __device__ __forceinline__ int st_prefix_segment(const StParams& p, int s, int& 
     return s < p.heavy_segments ? s * heavy : p.heavy_segments * heavy + (s - p.heavy_segments) * light;
 }
 
-// Units that a CTA takes of `units` in all.
-__device__ __forceinline__ int st_share(const StParams& p, int units) { return units > p.n_ctas ? (units - 1) / p.n_ctas + 1 : 1; }
+// Units that a CTA takes of `units` in all: a tile at least.
+__device__ __forceinline__ int st_share(const StParams& p, int units) { return max(units > 0 ? (units - 1) / p.n_ctas + 1 : 1, p.heavy_segments > 0 ? ST_HEAVY : ST_LIGHT); }
 
 // Next fragment of the stretch [u, end) of CTA `cta`; false when there is none.  It may be without a tile (none of the segment begins in the stretch).
 __device__ __forceinline__ bool st_next(const StParams& p, const int32_t* own_base, int cta, int& u, int end, StFragment& f) {
@@ -228,44 +227,13 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
         prefetch_tensormap(&tmap_q_own);
     }
     grid_wait();
-    // units of every session's own tokens, per part of its heads
-    const int per = (p.B + ST_THREADS - 1) / ST_THREADS, b0 = min(static_cast<int>(threadIdx.x) * per, p.B), b1 = min(b0 + per, p.B);
-    int mine = 0;
-    for (int b = b0; b < b1; ++b) {
-        bool bad;
-        const int64_t len = st_length(p, b, bad);
-        const int n = len > p.prefix ? st_units(static_cast<int>((len - p.own_start + KT - 1) / KT), ST_LIGHT) : 0;
-        sh->own_base[b] = n;
-        mine += n;
-        if (bad && blockIdx.x == 0) report(p.dev_status, JANUS_DEV_INDEX_OUT_OF_RANGE);
-    }
-    int own_units;
-    int at = block_exclusive_scan<ST_THREADS>(mine, sh->warp_sums, &own_units);
-    for (int b = b0; b < b1; ++b) {
-        const int n = sh->own_base[b];
-        sh->own_base[b] = at;
-        if (blockIdx.x == 0) p.own_base[b] = at;
-        at += n;
-    }
-    if (threadIdx.x == 0) {
-        sh->own_base[p.B] = own_units;
-        if (blockIdx.x == 0) p.own_base[p.B] = own_units;
-        // misaligned shared memory, or an earlier CTA that gave up on a wait
-        uint32_t flag = (smem_u32(smem) & 1023u) != 0u ? 1u : 0u;
-        if (flag != 0u) report(p.dev_status, JANUS_DEV_WAIT_TIMEOUT);
-        if (p.dev_status != nullptr && *reinterpret_cast<volatile int32_t*>(p.dev_status) == JANUS_DEV_WAIT_TIMEOUT) flag = 1u;
-        sh->abort = flag;
-    }
-    __syncwarp();
     if (warp == ST_QK_WARP) { tmem_alloc(smem_u32(&sh->tmem_base), 512); tmem_relinquish(); }
     tc_fence_before();
     __syncthreads();
     grid_launch_next();      // (tensor memory is allocated)
     tc_fence_after();
     const uint32_t tmem = sh->tmem_base;
-    const int units = p.prefix_units + own_units * p.n_kv * p.parts, share = st_share(p, units), cta = blockIdx.x;
-    int u = min(static_cast<int64_t>(share) * cta, static_cast<int64_t>(units));
-    const int end = min(static_cast<int64_t>(u) + share, static_cast<int64_t>(units));
+    const int cta = blockIdx.x;
     auto wait_warp = [](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(smem_u32(bar), parity)) != 0; };
     bool ok = true;
     StFragment f;
@@ -282,13 +250,10 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
         return f.last == 0;
     };
 
-    const bool start = sh->abort == 0u;
     // registers: 256 x 208 + 128 x 88 = 384 x 168, what the block was launched with; a raise waits until so many have been given up
     auto more_registers = [] { asm volatile("setmaxnreg.inc.sync.aligned.u32 208;"); };
     auto fewer_registers = [] { asm volatile("setmaxnreg.dec.sync.aligned.u32 88;"); };
-    if (!start) {
-        // nothing to do
-    } else if (warp >= ST_SOFTMAX_WARPS) {
+    if (warp >= ST_SOFTMAX_WARPS) {
     fewer_registers();      // all four warps: the softmax warps wait for what they give up
     if (warp == ST_COPY_WARP) {
         // ================================================================== copies
@@ -491,6 +456,43 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
         // Two places of 128 rows: a fragment of more rows takes both, others take them in turn.  Rows that a chunk or a segment does not have hold
         // whatever comes; nothing is read of what becomes of them.
         uint32_t n_q = 0u;
+        // units of every session's own tokens, per part of its heads: a lane adds up its own consecutive sessions, then the lanes' sums are scanned
+        const int per = (p.B + 31) / 32, b0 = min(lane * per, p.B), b1 = min(b0 + per, p.B);
+        // (nothing is done where shared memory is misaligned, or an earlier CTA of the launch gave up on a wait)
+        bool give_up = (smem_u32(smem) & 1023u) != 0u;
+        if (give_up) report(p.dev_status, JANUS_DEV_WAIT_TIMEOUT);
+        if (p.dev_status != nullptr && *reinterpret_cast<volatile int32_t*>(p.dev_status) == JANUS_DEV_WAIT_TIMEOUT) give_up = true;
+        int sum = 0;
+        for (int b = b0; b < b1; ++b) {
+            bool bad;
+            const int64_t len = st_length(p, b, bad);
+            const int n = len > p.prefix ? st_units(static_cast<int>((len - p.own_start + KT - 1) / KT), ST_LIGHT) : 0;
+            sh->own_base[b] = n;
+            sum += n;
+            if (bad && blockIdx.x == 0) report(p.dev_status, JANUS_DEV_INDEX_OUT_OF_RANGE);
+        }
+        int before = sum;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, before, d);
+            if (lane >= d) before += y;
+        }
+        const int own_units = __shfl_sync(0xffffffffu, before, 31);
+        before -= sum;
+        for (int b = b0; b < b1; ++b) {
+            const int n = sh->own_base[b];
+            sh->own_base[b] = before;
+            if (blockIdx.x == 0) p.own_base[b] = before;
+            before += n;
+        }
+        if (lane == 0) {
+            sh->own_base[p.B] = own_units;
+            if (blockIdx.x == 0) p.own_base[p.B] = own_units;
+        }
+        __syncwarp();
+        const int units = p.prefix_units + own_units * p.n_kv * p.parts, share = st_share(p, units);
+        int u = min(static_cast<int64_t>(share) * cta, static_cast<int64_t>(units));
+        const int end = __any_sync(0xffffffffu, give_up) ? u : min(static_cast<int64_t>(u) + share, static_cast<int64_t>(units));
         auto publish = [&]() {
             const bool more = st_next(p, sh->own_base, cta, u, end, f);
             const uint32_t i = n_fragment % ST_FRAGMENTS;
@@ -771,8 +773,17 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
 }
 
 // ---- merge: a block takes eight rows that lie one behind the other in the segments (128 bytes of every output at a time); its threads are
-// (row, four dims, share of the row's outputs), HERE fours of dims.  32 outputs of a row at a time: a warp works out their weights, then all threads add them up.
+// (row, four dims, share of the row's outputs), HERE fours of dims.  A thread loads maxima, sums and outputs of AT_ONCE fragments together.
 constexpr int SM_ROWS = 8;
+
+// x / d for d > 0 and a quotient below 2^20; inv = 1 / d, rounded.
+__device__ __forceinline__ int st_divide(int x, int d, float inv) {
+    int q = __float2int_rd(__int2float_rn(x) * inv);
+    const int r = x - q * d;
+    if (r < 0) --q;
+    if (r >= d) ++q;
+    return q;
+}
 
 // A row's outputs in a segment: one from every fragment (more than 128 rows), or one from each group of every fragment.
 struct SmPart {
@@ -780,114 +791,112 @@ struct SmPart {
     int64_t place;                       // of the first, in groups; step to the next
 };
 
-template <int DV, int HERE, int SHARES>
+template <int DV, int HERE, int SHARES, int AT_ONCE>
 __global__ void __launch_bounds__(SM_ROWS * HERE * SHARES) attn_shared_merge_kernel(const __grid_constant__ StParams p) {
     constexpr int CHUNKS = DV / 4;
     grid_launch_next();
     __shared__ SmPart parts_s[SM_ROWS][2];
-    __shared__ float weight[SM_ROWS][32], scale_s[SM_ROWS], sum_s[SM_ROWS], max_s[SM_ROWS];
+    __shared__ float2 ml_s[SHARES][SM_ROWS];
     __shared__ float4 acc_s[SHARES > 1 ? SHARES - 1 : 1][HERE][SM_ROWS];
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x;
     const float neg_inf = __int_as_float(0xff800000);
-    grid_wait();
+    const float inv_group = __frcp_rn(static_cast<float>(p.group));
     const int x_rows = p.B * p.group, blocks = (x_rows + SM_ROWS - 1) / SM_ROWS, h = blockIdx.x / blocks, x0 = (blockIdx.x - h * blocks) * SM_ROWS;
+    grid_wait();
     // a lane for each row's segment in the prefix, one for its own
     if (tid < 2 * SM_ROWS) {
         SmPart part = {};
-        const int x = x0 + (tid >> 1), b = x / p.group, g = x - b * p.group;
+        const int x = min(x0 + (tid >> 1), x_rows - 1), b = st_divide(x, p.group, inv_group), g = x - b * p.group;
+        // (all loads at once)
+        const int all = ld_input(p.own_base + p.B), base = ld_input(p.own_base + b), seg = ld_input(p.own_base + b + 1) - base;
         bool bad;
-        if (x < x_rows && st_length(p, b, bad) > 0) {
-            const int segments = p.n_kv * p.parts, share = st_share(p, p.prefix_units + ld_input(p.own_base + p.B) * segments), sub = g / ST_ROWS, c = b * p.parts + sub;
+        const int64_t len = st_length(p, b, bad);
+        if (x0 + (tid >> 1) < x_rows && len > 0) {
+            const int segments = p.n_kv * p.parts, share = st_share(p, p.prefix_units + all * segments), sub = g / ST_ROWS, c = b * p.parts + sub;
+            const float inv_share = __frcp_rn(static_cast<float>(share));
             if ((tid & 1) == 0 && p.prefix > 0) {
-                const int tile = c / (2 * p.per_tile), in_tile = c - tile * 2 * p.per_tile, half = in_tile >= p.per_tile ? 1 : 0, s = tile * p.n_kv + h;
+                const int tile = st_divide(c, 2 * p.per_tile, __frcp_rn(static_cast<float>(2 * p.per_tile))), in_tile = c - tile * 2 * p.per_tile;
+                const int half = in_tile >= p.per_tile ? 1 : 0, s = tile * p.n_kv + h;
                 int w;
-                const int u0 = st_prefix_segment(p, s, w), cta = u0 / share;
-                part.n = (u0 + st_units(p.prefix_tiles, w) - 1) / share - cta + 1;
+                const int u0 = st_prefix_segment(p, s, w), cta = st_divide(u0, share, inv_share);
+                part.n = st_divide(u0 + st_units(p.prefix_tiles, w) - 1, share, inv_share) - cta + 1;
                 part.place = 2 * (static_cast<int64_t>(cta) + s) + half;
                 part.step = 2;
                 if (s >= p.heavy_segments) { part.n *= 2; part.step = 1; }
                 part.row = (in_tile - half * p.per_tile) * p.chunk_rows + (g - sub * ST_ROWS);
             }
-            if ((tid & 1) != 0) {
-                const int base = ld_input(p.own_base + b), seg = ld_input(p.own_base + b + 1) - base;
-                if (seg > 0) {
-                    const int k = h * p.parts + sub, u0 = p.prefix_units + base * segments + k * seg, cta = u0 / share;
-                    part.n = 2 * ((u0 + seg - 1) / share - cta + 1);
-                    part.place = 2 * (static_cast<int64_t>(cta) + static_cast<int64_t>(b) * segments + k);
-                    part.step = 1;
-                    part.row = g - sub * ST_ROWS;
-                }
+            if ((tid & 1) != 0 && seg > 0) {
+                const int k = h * p.parts + sub, u0 = p.prefix_units + base * segments + k * seg, cta = st_divide(u0, share, inv_share);
+                part.n = 2 * (st_divide(u0 + seg - 1, share, inv_share) - cta + 1);
+                part.place = 2 * (static_cast<int64_t>(cta) + static_cast<int64_t>(b) * segments + k);
+                part.step = 1;
+                part.row = g - sub * ST_ROWS;
             }
         }
         parts_s[tid >> 1][tid & 1] = part;
     }
     __syncthreads();
     const int row = tid % SM_ROWS, here = tid / SM_ROWS % HERE, chunk = blockIdx.y * HERE + here, share = tid / (SM_ROWS * HERE);
-    int most = 0;
-#pragma unroll
-    for (int r = 0; r < SM_ROWS; ++r) most = max(most, parts_s[r][0].n + parts_s[r][1].n);
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float m = neg_inf, l = 0.f;          // of row `warp`: maximum so far, this lane's part of the sum
-    const bool weighs = warp < SM_ROWS;
-    const SmPart pre_w = parts_s[warp % SM_ROWS][0], own_w = parts_s[warp % SM_ROWS][1], pre = parts_s[row][0], own = parts_s[row][1];
-    auto left = [&](int i) {             // maximum and sum of output i of row `warp`
-        if (i < pre_w.n) return __ldcg(p.pre_ml + (pre_w.place + pre_w.step * i) * ST_ROWS + pre_w.row);
-        if (i < pre_w.n + own_w.n) return __ldcg(p.own_ml + (own_w.place + (i - pre_w.n)) * p.chunk_rows + own_w.row);
-        return make_float2(neg_inf, 0.f);
-    };
-    float2 next = make_float2(neg_inf, 0.f);
-    if (weighs) next = left(lane);
+    const SmPart pre = parts_s[row][0], own = parts_s[row][1];
+    const int n = pre.n + own.n;
+    const float2* const pre_ml = p.pre_ml + pre.place * ST_ROWS + pre.row;
+    const float2* const own_ml = p.own_ml + own.place * p.chunk_rows + own.row;
     const float4* const pre_o = reinterpret_cast<const float4*>(p.pre_o) + (pre.place * CHUNKS + chunk) * ST_ROWS + pre.row;
     const float4* const own_o = reinterpret_cast<const float4*>(p.own_o) + (own.place * CHUNKS + chunk) * p.chunk_rows + own.row;
-    const int64_t pre_step = static_cast<int64_t>(pre.step) * CHUNKS * ST_ROWS, own_step = static_cast<int64_t>(CHUNKS) * p.chunk_rows;
-    for (int i0 = 0; i0 < most; i0 += 32) {
-        if (weighs) {
-            const float2 v = next;
-            next = left(i0 + 32 + lane);
-            float top = fmaxf(m, v.x);
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float m = neg_inf, l = 0.f;
+    for (int i0 = share; i0 < n; i0 += SHARES * AT_ONCE) {
+        float2 v[AT_ONCE];
+        float4 o[AT_ONCE];
 #pragma unroll
-            for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-            const float safe = top == neg_inf ? 0.f : top, old = st_exp2(m - safe), f = st_exp2(v.x - safe);
-            const bool empty = v.x == neg_inf && v.y == 0.f;      // (a sum that is not a number counts)
-            l = l * old + (empty ? 0.f : f * v.y);
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const int i = i0 + k * SHARES, j = i - pre.n;
+            v[k] = make_float2(neg_inf, 0.f);
+            if (i < n) {
+                const int64_t step = i < pre.n ? static_cast<int64_t>(pre.step) * i * ST_ROWS : static_cast<int64_t>(j) * p.chunk_rows;
+                v[k] = __ldcg((i < pre.n ? pre_ml : own_ml) + step);
+                o[k] = __ldcg((i < pre.n ? pre_o : own_o) + step * CHUNKS);      // (whatever it is where the fragment has left nothing)
+            }
+        }
+        float top = m;
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) top = fmaxf(top, v[k].x);
+        const float safe = top == neg_inf ? 0.f : top, old = st_exp2(m - safe);
+        l *= old; acc.x *= old; acc.y *= old; acc.z *= old; acc.w *= old;
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            if (v[k].x == neg_inf && v[k].y == 0.f) continue;      // (a sum that is not a number counts)
+            const float f = st_exp2(v[k].x - safe);
+            l = fmaf(f, v[k].y, l);
+            acc.x = fmaf(f, o[k].x, acc.x); acc.y = fmaf(f, o[k].y, acc.y); acc.z = fmaf(f, o[k].z, acc.z); acc.w = fmaf(f, o[k].w, acc.w);
+        }
+        m = top;
+    }
+    if constexpr (SHARES > 1) {
+        if (here == 0) ml_s[share][row] = make_float2(m, l);
+        if (share > 0) acc_s[share - 1][here][row] = acc;
+        __syncthreads();
+        if (share == 0) {
+            float top = m;
+#pragma unroll
+            for (int i = 1; i < SHARES; ++i) top = fmaxf(top, ml_s[i][row].x);
+            const float safe = top == neg_inf ? 0.f : top, old = st_exp2(m - safe);
+            l *= old; acc.x *= old; acc.y *= old; acc.z *= old; acc.w *= old;
+#pragma unroll
+            for (int i = 1; i < SHARES; ++i) {
+                const float2 w = ml_s[i][row];
+                const float4 x = acc_s[i - 1][here][row];
+                const float f = st_exp2(w.x - safe);
+                l = fmaf(f, w.y, l);
+                acc.x = fmaf(f, x.x, acc.x); acc.y = fmaf(f, x.y, acc.y); acc.z = fmaf(f, x.z, acc.z); acc.w = fmaf(f, x.w, acc.w);
+            }
             m = top;
-            weight[warp][lane] = empty ? -1.f : f;
-            if (lane == 0) scale_s[warp] = old;
         }
-        __syncthreads();
-        if (i0 > 0) {
-            const float f0 = scale_s[row];
-            acc.x *= f0; acc.y *= f0; acc.z *= f0; acc.w *= f0;
-        }
-        const int count = min(32, pre.n + own.n - i0);
-#pragma unroll 8
-        for (int j = share; j < count; j += SHARES) {
-            const float f1 = weight[row][j];
-            const int i = i0 + j;
-            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (f1 >= 0.f || f1 != f1) o = __ldcg(i < pre.n ? pre_o + i * pre_step : own_o + (i - pre.n) * own_step);
-            acc.x = fmaf(f1, o.x, acc.x); acc.y = fmaf(f1, o.y, acc.y); acc.z = fmaf(f1, o.z, acc.z); acc.w = fmaf(f1, o.w, acc.w);
-        }
-        __syncthreads();
     }
-    if (weighs) {
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
-        if (lane == 0) { sum_s[warp] = l; max_s[warp] = m; }
-    }
-    if (SHARES > 1 && share > 0) acc_s[share - 1][here][row] = acc;
-    __syncthreads();
     const int x = x0 + row;
     if (share == 0 && x < x_rows) {
-#pragma unroll
-        for (int i = 0; i < SHARES - 1; ++i) {
-            const float4 v = acc_s[i][here][row];
-            acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
-        }
-        l = sum_s[row];
-        m = max_s[row];
         const float inv = l != 0.f ? 1.f / l : 0.f;        // (a NaN is a sum)
-        const int b = x / p.group;
+        const int b = st_divide(x, p.group, inv_group);
         const int64_t out = static_cast<int64_t>(b) * p.H_q + h * p.group + (x - b * p.group);
         *reinterpret_cast<uint2*>(p.out + out * DV + 4 * chunk) = make_uint2(st_pack_bf16x2(acc.x * inv, acc.y * inv), st_pack_bf16x2(acc.z * inv, acc.w * inv));
         if (p.lse != nullptr && chunk == 0) p.lse[out] = l != 0.f ? ((m == neg_inf ? 0.f : m) + log2f(l)) * 0.6931471805599453f : neg_inf;
@@ -1012,11 +1021,11 @@ static int st_launch(const SharedAttnArgs& a, StParams p, cudaStream_t stream) {
         CUtensorMap map_q, map_q_own;
         if (!st_tmap_q(&map_q, p.q, DQK, p.H_q, p.B, l.chunk_rows, l.per_tile) || !st_tmap_q(&map_q_own, p.q, DQK, p.H_q, p.B, l.chunk_rows, 1)) return JANUS_ERR_CUDA;
         JANUS_CUDA_CHECK(launch_kernel(attn_shared_kernel<DQK, DV>, dim3(p.n_ctas), ST_THREADS, C::SMEM, stream, 1, map_k, map_v, map_q, map_q_own, p));
-        // Few rows have many outputs each: eight shares of them, and the dims in several blocks (32 rows with 64 outputs each 7.1 us; one block 13.0).
-        // Many rows fill the SMs with a block for eight rows (3072 rows: 7.3 us; dims in several blocks 20.8).
+        // Few rows have many outputs each: eight shares of them, and the dims in several blocks, as long as those are resident at once.  Many rows fill the
+        // SMs with a block for eight rows.
         const int64_t blocks = (static_cast<int64_t>(p.B) * p.group + SM_ROWS - 1) / SM_ROWS * p.n_kv;
-        if (blocks <= ST_MAX_CTAS) JANUS_CUDA_CHECK(launch_kernel(attn_shared_merge_kernel<DV, 4, 8>, dim3(static_cast<unsigned>(blocks), DV / 16), 256, 0, stream, 1, p));
-        else JANUS_CUDA_CHECK(launch_kernel(attn_shared_merge_kernel<DV, DV / 4, 128 / DV>, dim3(static_cast<unsigned>(blocks)), 256, 0, stream, 1, p));
+        if (blocks * (DV / 16) <= 4 * ST_MAX_CTAS) JANUS_CUDA_CHECK(launch_kernel(attn_shared_merge_kernel<DV, 4, 8, 4>, dim3(static_cast<unsigned>(blocks), DV / 16), 256, 0, stream, 1, p));
+        else JANUS_CUDA_CHECK(launch_kernel(attn_shared_merge_kernel<DV, DV / 4, 128 / DV, 8>, dim3(static_cast<unsigned>(blocks)), 256, 0, stream, 1, p));
     }
     return JANUS_OK;
 }

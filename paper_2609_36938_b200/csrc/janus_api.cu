@@ -52,7 +52,7 @@ bool sparse_attn_latent_tc_supported(int M, int H_q, int d_qk, const void* k_poo
                                      int64_t tok_stride, int n_kv_heads, int d_v, int k);
 int launch_sparse_attn_latent_tc(const void* q, int M, const void* pool, int64_t page_stride, int64_t tok_stride, const int32_t* idx, int k,
                                  int page_size, const int32_t* page_table, int64_t n_logical_pages, const int64_t* table_offsets,
-                                 float softmax_scale, void* out, float* lse, int32_t* dev_status, cudaStream_t stream, bool exact_sum = false);
+                                 float softmax_scale, void* out, float* lse, int32_t* dev_status, cudaStream_t stream);
 
 // Host-side checks shared by the entry points that take indexer operands.  JANUS_OK also for empty problems.
 int validate_indexer_args(const void* q_idx, int64_t q_stride_tok, const void* k_idx, int64_t k_stride_tok, const float* w,
@@ -159,17 +159,6 @@ static int sparse_attn_dispatch(const void* q, int M, int H_q, int d_qk, const v
                                         page_size, page_table, n_logical_pages, table_offsets, softmax_scale, out, lse, dev_status, stream);
     return launch_sparse_attn_generic(q, M, H_q, d_qk, k_pool, v_pool, page_stride, tok_stride, head_stride, page_stride, tok_stride, head_stride, n_kv_heads,
                                       d_v, idx, k, page_size, page_table, n_logical_pages, table_offsets, softmax_scale, out, lse, dev_status, stream);
-}
-// All tokens of a session as its selection (janus_attn_decode_shared, which has checked its arguments): layouts without a kernel of its own.
-int sparse_attn_listed(const void* q, int M, int H_q, int d_qk, const void* k_pool, const void* v_pool, int64_t page_stride, int64_t tok_stride,
-                       int64_t head_stride, int64_t v_page_stride, int64_t v_tok_stride, int64_t v_head_stride, int n_kv_heads, int d_v, const int32_t* idx, int k,
-                       int page_size, const int32_t* page_tables, const int64_t* table_offsets, float softmax_scale, void* out, float* lse, int32_t* dev_status,
-                       cudaStream_t stream) {
-    if (sparse_attn_latent_tc_supported(M, H_q, d_qk, k_pool, v_pool, page_stride, tok_stride, n_kv_heads, d_v, k))
-        return launch_sparse_attn_latent_tc(q, M, k_pool, page_stride, tok_stride, idx, k, page_size, page_tables, 0, table_offsets, softmax_scale, out, lse,
-                                            dev_status, stream, true);
-    return launch_sparse_attn_generic(q, M, H_q, d_qk, k_pool, v_pool, page_stride, tok_stride, head_stride, v_page_stride, v_tok_stride, v_head_stride, n_kv_heads,
-                                      d_v, idx, k, page_size, page_tables, 0, table_offsets, softmax_scale, out, lse, dev_status, stream);
 }
 }  // namespace janus
 

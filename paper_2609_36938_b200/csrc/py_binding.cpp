@@ -389,10 +389,12 @@ T* vec(const at::Tensor& t, at::ScalarType type, int64_t n, const char* name) {
 }
 // Tensors whose memory lies on the current device, whose stream and status word the call takes.
 void here(std::initializer_list<const at::Tensor*> list) {
+    int current = -1;
     for (const at::Tensor* t : list)
         if (t->defined()) {
-            ptr(*t);      // (refuses host tensors before the device is asked for)
-            if (t->get_device() != c10::cuda::current_device()) fail(janus_error, "a tensor is not on the current device");
+            if (!t->is_cuda()) fail(janus_error, "expected a CUDA tensor (the library takes device pointers)");
+            if (current < 0) current = c10::cuda::current_device();      // (after the first look: without a device it is torch that fails)
+            if (t->get_device() != current) fail(janus_error, "a tensor is not on the current device");
         }
 }
 int32_t* i32_vec(const at::Tensor& t, int64_t n, const char* name) { return vec<int32_t>(t, at::kInt, n, name); }

@@ -115,6 +115,8 @@ struct LpParams {
     uint16_t* out;
     float* lse;
     int M;
+    const int32_t* rows;            // PIECES: number of rows, at most M, and their query tokens
+    const int32_t* token_of;
     int32_t* dev_status;
 };
 
@@ -208,8 +210,9 @@ __device__ __forceinline__ void lp_merge_splits(const LpParams& p, int t, int s,
 // SPLIT = false: clusters of two CTAs, persistent over tokens.  SPLIT = true: a cluster of 2 n CTAs takes one token, pair s of it
 // the tiles [s, s + 1) * n_tiles / n, and the pairs' outputs are merged through distributed shared memory at the end.
 // ROWS = true: the pool's rows lie at whole multiples of one stride and those of K are gathered by number; false: by address.
-// EXACT_SUM = true: the row sum adds the probabilities before they are rounded (below).
-template <bool SPLIT, bool ROWS, bool EXACT_SUM>
+// PIECES = true: a row of the selection is a piece of a query token's keys; how many there are and which token each belongs to lies in device memory
+// (p.rows, p.token_of), and the row sum adds the probabilities before they are rounded (below).
+template <bool SPLIT, bool ROWS, bool PIECES>
 __global__ void __launch_bounds__(LP_THREADS, 1) sparse_attn_latent_pair_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_pool,
                                                                               const LpParams p) {
     extern __shared__ __align__(1024) unsigned char smem[];
@@ -226,11 +229,9 @@ __global__ void __launch_bounds__(LP_THREADS, 1) sparse_attn_latent_pair_kernel(
     // persistent: cluster `cid` handles tokens cid, cid + n_clusters, ...; tiles are counted over all of them
     const int n_split = SPLIT ? static_cast<int>(cluster_nctarank() >> 1) : 1;
     const int cid = blockIdx.x / (2 * n_split), n_clusters = gridDim.x / (2 * n_split);
-    const int n_my = cid < p.M ? (p.M - cid + n_clusters - 1) / n_clusters : 0;     // SPLIT: one cluster per token, so 1
     const int all_tiles = (p.k + LP_TILE - 1) / LP_TILE;
     const int tile0 = SPLIT ? static_cast<int>(rank >> 1) * all_tiles / n_split : 0;
     const int n_tiles = SPLIT ? (static_cast<int>(rank >> 1) + 1) * all_tiles / n_split - tile0 : all_tiles;
-    const int total = n_my * n_tiles;
 
     if (SPLIT && threadIdx.x < LP_OWN) sh->split_l[threadIdx.x] = -1.f;
     if (threadIdx.x == 0) {
@@ -252,6 +253,10 @@ __global__ void __launch_bounds__(LP_THREADS, 1) sparse_attn_latent_pair_kernel(
         fence_mbar_init();
     }
     grid_wait();
+    int n_rows = p.M;
+    if constexpr (PIECES) n_rows = min(ld_input(p.rows), p.M);
+    const int n_my = cid < n_rows ? (n_rows - cid + n_clusters - 1) / n_clusters : 0;     // SPLIT: one cluster per token, so 1
+    const int total = n_my * n_tiles;
     cluster_wait();                                // every CTA of the cluster runs: its shared memory may be written
     if (threadIdx.x == 0) {
         // start-up agreement: if this CTA should not start (misaligned shared memory, or an earlier CTA of the launch gave
@@ -505,7 +510,9 @@ __global__ void __launch_bounds__(LP_THREADS, 1) sparse_attn_latent_pair_kernel(
         };
         // queries of this CTA's heads, token `it`: atoms 0-5 through the ring, atoms 6-8 to their place (warp 0; plain copies of boxes)
         auto fill_q = [&](int it) {
-            const int y = (cid + it * n_clusters) * LP_HEADS + LP_OWN * static_cast<int>(c);
+            int token = cid + it * n_clusters;
+            if constexpr (PIECES) token = ld_input(p.token_of + token);
+            const int y = token * LP_HEADS + LP_OWN * static_cast<int>(c);
             for (int a = 0; a < LP_QPARTS; ++a) {
                 uint64_t *const full = &sh->k_full[unit_slot], *const empty = &sh->k_empty[unit_slot];
                 // ROWS: only the warp that fills the unit waits for its place.  The unit lands and its place is freed again without the others, so that
@@ -692,7 +699,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) sparse_attn_latent_pair_kernel(
             }
             const float neg_m = (m_ref == neg_inf) ? 0.f : -m_ref;
             // P is rounded to bf16 (one pack instruction per pair); the row sum adds the very same rounded values, so the
-            // normalisation stays consistent and the log-sum-exp is not biased.  With EXACT_SUM it adds them as they were: over all tokens of a
+            // normalisation stays consistent and the log-sum-exp is not biased.  With PIECES it adds them as they were: over all tokens of a
             // session the rounding of single probabilities leaves 3e-5 in the log-sum-exp, and in the output what its own rounding hides.
             uint32_t pk[16];
             float2 ts[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
@@ -701,7 +708,7 @@ __global__ void __launch_bounds__(LP_THREADS, 1) sparse_attn_latent_pair_kernel(
             for (int j = 0; j < 16; ++j) {
                 const float2 e = ffma2(x[j], sc2, nm2), pr = make_float2(lp_exp2(e.x), lp_exp2(e.y));
                 pk[j] = lp_pack_bf16x2(pr.x, pr.y);       // low half = bf16(p of key 2j), high half = bf16(p of key 2j+1)
-                ts[j & 3] = fadd2(ts[j & 3], EXACT_SUM ? pr : make_float2(__uint_as_float(pk[j] << 16), __uint_as_float(pk[j] & 0xffff0000u)));
+                ts[j & 3] = fadd2(ts[j & 3], PIECES ? pr : make_float2(__uint_as_float(pk[j] << 16), __uint_as_float(pk[j] & 0xffff0000u)));
             }
             const float2 t4 = fadd2(fadd2(ts[0], ts[1]), fadd2(ts[2], ts[3]));
             l_sum += t4.x + t4.y;
@@ -805,12 +812,8 @@ static int lp_resident_clusters(int dev, size_t smem, int (&n)[LP_MAX_SPLIT + 1]
         larger(sparse_attn_latent_pair_kernel<true, true, false>);
         larger(sparse_attn_latent_pair_kernel<false, false, true>);
         larger(sparse_attn_latent_pair_kernel<false, true, true>);
-        larger(sparse_attn_latent_pair_kernel<true, false, true>);
-        larger(sparse_attn_latent_pair_kernel<true, true, true>);
         wider(sparse_attn_latent_pair_kernel<true, false, false>);
         wider(sparse_attn_latent_pair_kernel<true, true, false>);
-        wider(sparse_attn_latent_pair_kernel<true, false, true>);
-        wider(sparse_attn_latent_pair_kernel<true, true, true>);
         return e;
     }));
     std::lock_guard<std::mutex> lock(mu);
@@ -836,9 +839,10 @@ static int lp_resident_clusters(int dev, size_t smem, int (&n)[LP_MAX_SPLIT + 1]
     return JANUS_OK;
 }
 
-int launch_sparse_attn_latent_tc(const void* q, int M, const void* pool, int64_t page_stride, int64_t tok_stride, const int32_t* idx, int k,
-                                 int page_size, const int32_t* page_table, int64_t n_logical_pages, const int64_t* table_offsets,
-                                 float softmax_scale, void* out, float* lse, int32_t* dev_status, cudaStream_t stream, bool exact_sum) {
+// `rows` (and `token_of`, `n_tokens`): the selection's rows are pieces of the tokens' keys (PIECES above), M of them at most; else NULL.
+static int lp_launch(const void* q, int n_tokens, int M, const void* pool, int64_t page_stride, int64_t tok_stride, const int32_t* idx, int k,
+                     int page_size, const int32_t* page_table, int64_t n_logical_pages, const int64_t* table_offsets,
+                     float softmax_scale, void* out, float* lse, int32_t* dev_status, cudaStream_t stream, const int32_t* rows, const int32_t* token_of) {
     LpParams p;
     p.q = static_cast<const uint16_t*>(q);
     p.pool = static_cast<const uint16_t*>(pool);
@@ -859,6 +863,7 @@ int launch_sparse_attn_latent_tc(const void* q, int M, const void* pool, int64_t
     p.out = static_cast<uint16_t*>(out);
     p.lse = lse;
     p.M = M;
+    p.rows = rows; p.token_of = token_of;
     p.dev_status = dev_status;
     constexpr size_t smem = LP_SMEM_TILES + 2 * LP_P_BYTES + LP_Q_BYTES + sizeof(LpShared);
     static_assert(smem <= 227 * 1024, "shared memory");
@@ -875,7 +880,7 @@ int launch_sparse_attn_latent_tc(const void* q, int M, const void* pool, int64_t
     const int all_tiles = (k + LP_TILE - 1) / LP_TILE;
     int split = 1;
     double best = 0.;
-    for (int n = 1; n <= LP_MAX_SPLIT && n <= all_tiles; ++n) {
+    for (int n = 1; n <= (rows != nullptr ? 1 : LP_MAX_SPLIT) && n <= all_tiles; ++n) {
         if (n_resident[n] <= 0) break;
         const int waves = (M + n_resident[n] - 1) / n_resident[n];
         const double tiles = ((all_tiles + n - 1) / n) * 1.5;
@@ -887,19 +892,33 @@ int launch_sparse_attn_latent_tc(const void* q, int M, const void* pool, int64_t
     // Rows are gathered by number where the distance of the pages is a multiple of that of the tokens, as it is in any pool without
     // padding between pages (740 x 2048: 322 us; by address 333).
     CUtensorMap map = {}, map_q;
-    if (!make_tmap_2d_sw128(&map_q, q, 2, static_cast<uint64_t>(M) * LP_HEADS, LP_DQK, static_cast<uint64_t>(LP_DQK) * 2, LP_OWN, 64)) return JANUS_ERR_CUDA;
-    const bool rows = page_stride >= 0 && page_stride % tok_stride == 0 &&
+    if (!make_tmap_2d_sw128(&map_q, q, 2, static_cast<uint64_t>(n_tokens) * LP_HEADS, LP_DQK, static_cast<uint64_t>(LP_DQK) * 2, LP_OWN, 64)) return JANUS_ERR_CUDA;
+    const bool by_number = page_stride >= 0 && page_stride % tok_stride == 0 &&
                       make_tmap_2d_sw128(&map, pool, 2, 0x7fffffffu, LP_DQK, static_cast<uint64_t>(tok_stride) * 2, 1, 64);
     const int cluster = 2 * split;
     auto launch = [&](auto kernel) { return launch_kernel(kernel, grid, LP_THREADS, smem, stream, cluster, map_q, map, p); };
-    auto pick = [&](auto exact) {
-        constexpr bool E = decltype(exact)::value;
-        if (split > 1) return rows ? launch(sparse_attn_latent_pair_kernel<true, true, E>) : launch(sparse_attn_latent_pair_kernel<true, false, E>);
-        return rows ? launch(sparse_attn_latent_pair_kernel<false, true, E>) : launch(sparse_attn_latent_pair_kernel<false, false, E>);
-    };
-    const cudaError_t e = exact_sum ? pick(std::true_type{}) : pick(std::false_type{});
+    cudaError_t e;
+    if (rows != nullptr) e = by_number ? launch(sparse_attn_latent_pair_kernel<false, true, true>) : launch(sparse_attn_latent_pair_kernel<false, false, true>);
+    else if (split > 1) e = by_number ? launch(sparse_attn_latent_pair_kernel<true, true, false>) : launch(sparse_attn_latent_pair_kernel<true, false, false>);
+    else e = by_number ? launch(sparse_attn_latent_pair_kernel<false, true, false>) : launch(sparse_attn_latent_pair_kernel<false, false, false>);
     JANUS_CUDA_CHECK(e);
     return JANUS_OK;
+}
+
+int launch_sparse_attn_latent_tc(const void* q, int M, const void* pool, int64_t page_stride, int64_t tok_stride, const int32_t* idx, int k,
+                                 int page_size, const int32_t* page_table, int64_t n_logical_pages, const int64_t* table_offsets,
+                                 float softmax_scale, void* out, float* lse, int32_t* dev_status, cudaStream_t stream) {
+    return lp_launch(q, M, M, pool, page_stride, tok_stride, idx, k, page_size, page_table, n_logical_pages, table_offsets, softmax_scale, out, lse, dev_status, stream,
+                     nullptr, nullptr);
+}
+
+// Keys of n_tokens query tokens in pieces of k: piece r belongs to token token_of[r] and has its own page table and outputs; *rows of them (device), at
+// most max_rows.
+int launch_latent_pieces(const void* q, int n_tokens, int max_rows, const int32_t* rows, const int32_t* token_of, const void* pool, int64_t page_stride,
+                         int64_t tok_stride, const int32_t* idx, int k, int page_size, const int32_t* page_tables, const int64_t* table_offsets,
+                         float softmax_scale, void* out, float* lse, int32_t* dev_status, cudaStream_t stream) {
+    return lp_launch(q, n_tokens, max_rows, pool, page_stride, tok_stride, idx, k, page_size, page_tables, 0, table_offsets, softmax_scale, out, lse, dev_status, stream,
+                     rows, token_of);
 }
 
 }  // namespace janus
