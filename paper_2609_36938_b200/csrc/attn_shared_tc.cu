@@ -128,6 +128,15 @@ __device__ __forceinline__ int st_units(int tiles, int w) { return tiles * w + S
 // Tiles of a segment that begin before its unit x.
 __device__ __forceinline__ int st_tiles(int x, int w) { return x <= ST_SEGMENT ? 0 : (x - ST_SEGMENT + w - 1) / w; }
 
+// x / d for d > 0 and a quotient below 2^20; inv = 1 / d, rounded.
+__device__ __forceinline__ int st_divide(int x, int d, float inv) {
+    int q = __float2int_rd(__int2float_rn(x) * inv);
+    const int r = x - q * d;
+    if (r < 0) --q;
+    if (r >= d) ++q;
+    return q;
+}
+
 // First unit of prefix segment s, and the units of its tiles.
 __device__ __forceinline__ int st_prefix_segment(const StParams& p, int s, int& w) {
     const int heavy = st_units(p.prefix_tiles, ST_HEAVY), light = st_units(p.prefix_tiles, ST_LIGHT);
@@ -144,13 +153,15 @@ __device__ __forceinline__ bool st_next(const StParams& p, const int32_t* own_ba
         int u0, w, tiles;
         if (u < p.prefix_units) {
             const int heavy = st_units(p.prefix_tiles, ST_HEAVY), all_heavy = p.heavy_segments * heavy;
-            const int s = u < all_heavy ? u / heavy : p.heavy_segments + (u - all_heavy) / st_units(p.prefix_tiles, ST_LIGHT);
+            const int each = u < all_heavy ? heavy : st_units(p.prefix_tiles, ST_LIGHT), from = u < all_heavy ? 0 : all_heavy;
+            const int s = st_divide(u - from, each, __frcp_rn(static_cast<float>(each))) + (u < all_heavy ? 0 : p.heavy_segments);
+            const int tile = st_divide(s, p.n_kv, __frcp_rn(static_cast<float>(p.n_kv)));
             u0 = st_prefix_segment(p, s, w);
             tiles = p.prefix_tiles;
             f.prefix = true;
             f.heavy = s < p.heavy_segments;
-            f.h = s % p.n_kv;
-            f.c0 = s / p.n_kv * 2 * p.per_tile;
+            f.h = s - tile * p.n_kv;
+            f.c0 = tile * 2 * p.per_tile;
             f.rows = min(p.per_tile, p.chunks - f.c0) * p.chunk_rows;
             f.rows2 = f.heavy ? min(p.per_tile, p.chunks - f.c0 - p.per_tile) * p.chunk_rows : 0;
             f.b = 0;
@@ -163,12 +174,12 @@ __device__ __forceinline__ bool st_next(const StParams& p, const int32_t* own_ba
                 if (own_base[mid] * parts <= v) lo = mid;
                 else hi = mid;
             }
-            const int seg = own_base[lo + 1] - own_base[lo], part = (v - own_base[lo] * parts) / seg;
+            const int seg = own_base[lo + 1] - own_base[lo], part = st_divide(v - own_base[lo] * parts, seg, __frcp_rn(static_cast<float>(seg)));
             u0 = p.prefix_units + own_base[lo] * parts + part * seg;
             w = ST_LIGHT;
             tiles = (seg - ST_SEGMENT) / ST_LIGHT;
             f.prefix = f.heavy = false;
-            f.h = part / p.parts;
+            f.h = p.parts == 1 ? part : part / p.parts;
             f.c0 = lo * p.parts + (part - f.h * p.parts);
             f.rows = p.chunk_rows;
             f.rows2 = 0;
@@ -311,33 +322,36 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
             const int head = f.h;
             const int64_t p0 = base + static_cast<int64_t>(t) * KT;
             const int lo = !f.prefix && p.prefix > p0 ? static_cast<int>(p.prefix - p0) : 0, hi = len - p0 < KT ? static_cast<int>(len - p0) : KT;
-            uint32_t words[4] = {0u, 0u, 0u, 0u};
+            bool there[MOST], whole = lo == 0 && hi == KT;
 #pragma unroll
             for (int j = 0; j < MOST; ++j) {
-                const int i = lane + 32 * j;
-                const bool there = wanted[j] && id[j] >= 0 && id[j] < p.n_phys;
-                missing |= wanted[j] && !there;
-                page[j] = there ? id[j] : p.n_phys;
+                there[j] = wanted[j] && id[j] >= 0 && id[j] < p.n_phys;
+                missing |= wanted[j] && !there[j];
+                page[j] = there[j] ? id[j] : p.n_phys;
                 page_row[j] = row[j];
-                if (there)
-#pragma unroll
-                    for (int w = 0; w < KT / 32; ++w) {
-                        const int from = max(max(i * p.box, lo) - 32 * w, 0), to = min(min((i + 1) * p.box, hi) - 32 * w, 32);
-                        if (from < to) words[w] |= (to - from == 32 ? 0xffffffffu : ((1u << (to - from)) - 1u) << from);
-                    }
+                whole = whole && (there[j] || lane + 32 * j >= boxes);
             }
-            bool whole = true;
+            whole = __all_sync(0xffffffffu, whole) != 0;
+            uint32_t words[KT / 32];
+            if (!whole) {
 #pragma unroll
-            for (int w = 0; w < KT / 32; ++w) {
-                words[w] = __reduce_or_sync(0xffffffffu, words[w]);
-                whole = whole && words[w] == 0xffffffffu;
+                for (int w = 0; w < KT / 32; ++w) {
+                    uint32_t bits = 0u;
+#pragma unroll
+                    for (int j = 0; j < MOST; ++j) {
+                        const int i = lane + 32 * j, from = max(max(i * p.box, lo) - 32 * w, 0), to = min(min((i + 1) * p.box, hi) - 32 * w, 32);
+                        if (there[j] && from < to) bits |= to - from == 32 ? 0xffffffffu : ((1u << (to - from)) - 1u) << from;
+                    }
+                    words[w] = __reduce_or_sync(0xffffffffu, bits);
+                }
             }
             if (missing) report(p.dev_status, JANUS_DEV_INDEX_OUT_OF_RANGE);
             if (lane == 0) {
                 const uint32_t n = tc % ST_INFO;
                 sh->partial[n] = whole ? 0u : 1u;
+                if (!whole)
 #pragma unroll
-                for (int w = 0; w < 4; ++w) sh->mask[n][w] = words[w];
+                    for (int w = 0; w < KT / 32; ++w) sh->mask[n][w] = words[w];
                 mbar_arrive(smem_u32(&sh->info_full[n]));
             }
             __syncwarp();
@@ -459,9 +473,7 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
         // units of every session's own tokens, per part of its heads: a lane adds up its own consecutive sessions, then the lanes' sums are scanned
         const int per = (p.B + 31) / 32, b0 = min(lane * per, p.B), b1 = min(b0 + per, p.B);
         // (nothing is done where shared memory is misaligned, or an earlier CTA of the launch gave up on a wait)
-        bool give_up = (smem_u32(smem) & 1023u) != 0u;
-        if (give_up) report(p.dev_status, JANUS_DEV_WAIT_TIMEOUT);
-        if (p.dev_status != nullptr && *reinterpret_cast<volatile int32_t*>(p.dev_status) == JANUS_DEV_WAIT_TIMEOUT) give_up = true;
+        const int32_t status = p.dev_status != nullptr ? *reinterpret_cast<volatile int32_t*>(p.dev_status) : 0;
         int sum = 0;
         for (int b = b0; b < b1; ++b) {
             bool bad;
@@ -471,6 +483,9 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
             sum += n;
             if (bad && blockIdx.x == 0) report(p.dev_status, JANUS_DEV_INDEX_OUT_OF_RANGE);
         }
+        bool give_up = (smem_u32(smem) & 1023u) != 0u;
+        if (give_up) report(p.dev_status, JANUS_DEV_WAIT_TIMEOUT);
+        give_up = give_up || status == JANUS_DEV_WAIT_TIMEOUT;
         int before = sum;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -775,15 +790,6 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
 // ---- merge: a block takes eight rows that lie one behind the other in the segments (128 bytes of every output at a time); its threads are
 // (row, four dims, share of the row's outputs), HERE fours of dims.  A thread loads maxima, sums and outputs of AT_ONCE fragments together.
 constexpr int SM_ROWS = 8;
-
-// x / d for d > 0 and a quotient below 2^20; inv = 1 / d, rounded.
-__device__ __forceinline__ int st_divide(int x, int d, float inv) {
-    int q = __float2int_rd(__int2float_rn(x) * inv);
-    const int r = x - q * d;
-    if (r < 0) --q;
-    if (r >= d) ++q;
-    return q;
-}
 
 // A row's outputs in a segment: one from every fragment (more than 128 rows), or one from each group of every fragment.
 struct SmPart {
