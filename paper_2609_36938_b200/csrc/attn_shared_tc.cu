@@ -118,7 +118,7 @@ struct StParams {
 };
 
 // The line counts units: so many for a tile of more than 128 rows, for one of fewer, and for what a segment costs besides its tiles.
-constexpr int ST_HEAVY = 8, ST_LIGHT = 6, ST_SEGMENT = 10;
+constexpr int ST_HEAVY = 8, ST_LIGHT = 8, ST_SEGMENT = 12;
 
 // Lanes that share the keys of a row: where rows are so few that there are lanes for `most` of each, every one takes a slice of a tile's keys, with a
 // maximum, a sum and an output of its own until the fragment ends.  Lane i holds copy i / (128 / copies), row i % (128 / copies).
