@@ -366,7 +366,8 @@ int janus_sparse_attn_decode(const void* q, int B, int H_q, int d_qk,
  *                  at row key_offsets[b] (given with it; -1 where slots is -1)
  *   counts         [3] int64 out: pages taken, table entries, rows; the true numbers where a capacity was exceeded
  *
- * cached_lens is what janus_page_demand_batch takes as demand_limits.  An entry of length 0 stands empty.  Where lists are too short (free
+ * No output shares memory with an input or another output (JANUS_ERR_INVALID_ARG): a step's kv_lens may be the next step's cached_lens, which
+ * then writes to other buffers.  cached_lens is what janus_page_demand_batch takes as demand_limits.  An entry of length 0 stands empty.  Where lists are too short (free
  * pages, page_tables, rows, or a session longer than width * p) the call reports JANUS_DEV_CAPACITY_EXCEEDED: a page that could not be
  * taken, and the slot of a token without a page, is -1, offsets and lengths are cut back to what is there.  A negative length counts as 0, and a
  * page id outside [0, n_phys_pages) as -1, with JANUS_DEV_INDEX_OUT_OF_RANGE.  B <= 8192 and B * width < 2^31, else JANUS_ERR_UNSUPPORTED.
@@ -443,7 +444,9 @@ int janus_rope_append(const void* q, int64_t q_row_stride, int64_t q_head_stride
  *
  * A row none of whose logits is above -inf gives zeros.  Tokens whose page is missing or outside [0, n_phys_pages) are skipped, a length
  * below P empties its entry and one above max_len is cut back, each with JANUS_DEV_INDEX_OUT_OF_RANGE.  softmax_scale > 0.  d_qk and d_v
- * multiples of 8, d_qk <= 576, d_v <= 512, H_q a multiple of n_kv_heads; bases and strides on 16 bytes.
+ * multiples of 8, d_qk <= 576, d_v <= 512, H_q a multiple of n_kv_heads; bases and strides on 16 bytes, strides of axes longer than one
+ * positive; B <= 65535.  A tensor-core kernel serves keys of 64, 128 or 192 dims with values of 64 or 128 in any grouping; the latent shape (and,
+ * slowly, any other) goes through the sparse kernels with all tokens listed in the workspace.
  */
 size_t janus_attn_decode_shared_workspace_size(int B, int H_q, int d_qk, int n_kv_heads, int d_v, int page_size,
                                                int64_t prefix_len, int64_t max_len);

@@ -366,7 +366,8 @@ def janus_batch_plan(cached_lens: torch.Tensor, new_lens: torch.Tensor, block_ta
     """Page tables, rows, positions and cache places of a step from the lengths of its sessions (int64 [B] tensors on the device).
     block_tables [B, width] int32 holds the pages of the cached tokens; the further pages come from the beginning of free_pages and are
     written behind them.  key_offsets (int64 [B] or longer): also key_rows, the places of the indexer keys.  Returns a dict of device
-    tensors; the counts stay on the device (no host sync).  ``out``: buffers from batch_plan_buffers()."""
+    tensors; the counts stay on the device (no host sync).  ``out``: buffers from batch_plan_buffers(), none of which may be an input: a loop that
+    takes kv_lens of one step as cached_lens of the next keeps two sets."""
     if out is None:
         if table_capacity is None:
             table_capacity = block_tables.shape[0] * block_tables.shape[1]

@@ -235,6 +235,18 @@ extern "C" int janus_batch_plan(const int64_t* cached_lens, const int64_t* new_l
     if ((n_free > 0 && !free_pages) || (table_capacity > 0 && !page_tables)) return JANUS_ERR_INVALID_ARG;
     if (max_rows > 0 && (!row_sessions || !positions || !slots)) return JANUS_ERR_INVALID_ARG;
     if ((key_rows != nullptr) != (key_offsets != nullptr) && max_rows > 0) return JANUS_ERR_INVALID_ARG;
+    // What is written shares no memory with anything else: every CTA reads all lengths by itself, at no set time.
+    const int64_t table_bytes = B > 0 ? ((B - 1) * block_ld + width) * 4 : 0, n8 = 8 * static_cast<int64_t>(B);
+    const struct { const void* at; int64_t bytes; bool written; } memory[] = {
+        {row_offsets, n8 + 8, true}, {table_offsets, n8 + 8, true}, {counts, 24, true}, {kv_lens, n8, true}, {page_tables, 4 * table_capacity, true},
+        {row_sessions, 4 * max_rows, true}, {positions, 8 * max_rows, true}, {slots, 8 * max_rows, true}, {key_rows, 8 * max_rows, true}, {block_tables, table_bytes, true},
+        {cached_lens, n8, false}, {new_lens, n8, false}, {key_offsets, n8, false}, {free_pages, 4 * n_free, false}};
+    for (const auto& x : memory)
+        for (const auto& y : memory) {
+            if (&x == &y || !x.written || x.at == nullptr || y.at == nullptr || x.bytes <= 0 || y.bytes <= 0) continue;
+            const uintptr_t a = reinterpret_cast<uintptr_t>(x.at), b = reinterpret_cast<uintptr_t>(y.at);
+            if (a < b + static_cast<uint64_t>(y.bytes) && b < a + static_cast<uint64_t>(x.bytes)) return JANUS_ERR_INVALID_ARG;
+        }
     BpParams p;
     p.cached = cached_lens; p.fresh = new_lens;
     p.B = B; p.page_size = page_size;

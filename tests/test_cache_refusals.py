@@ -21,16 +21,23 @@ def lib():
 
 
 def test_batch_plan_refusals(lib):
+    names = ("cached", "new", "tables", "free", "ro", "kv", "to", "pt", "rs", "pos", "slots", "counts", "other")
+    at = {n: ctypes.c_void_p(0x10000 * (i + 1)) for i, n in enumerate(names)}      # each in memory of its own
+
     def call(**kw):
-        a = dict(cached=FAKE, new=FAKE, B=4, page=64, tables=FAKE, ld=16, width=16, free=FAKE, n_free=8, n_phys=100, key=None, ro=FAKE, kv=FAKE, to=FAKE, pt=FAKE,
-                 cap=64, rs=FAKE, pos=FAKE, slots=FAKE, kr=None, rows=8, counts=FAKE)
+        a = dict({n: at[n] for n in names}, B=4, page=64, ld=16, width=16, n_free=8, n_phys=100, key=None, cap=64, kr=None, rows=8)
         a.update(kw)
         return lib.janus_batch_plan(a["cached"], a["new"], a["B"], a["page"], a["tables"], a["ld"], a["width"], a["free"], a["n_free"], a["n_phys"], a["key"], a["ro"],
                                     a["kv"], a["to"], a["pt"], a["cap"], a["rs"], a["pos"], a["slots"], a["kr"], a["rows"], a["counts"], None, None)
 
     for bad in (dict(B=-1), dict(page=0), dict(ld=15), dict(width=-1), dict(n_free=-1), dict(cap=-1), dict(rows=-1), dict(n_phys=-1), dict(cached=None),
                 dict(new=None), dict(tables=None), dict(free=None), dict(ro=None), dict(kv=None), dict(to=None), dict(pt=None), dict(rs=None), dict(pos=None),
-                dict(slots=None), dict(counts=None), dict(key=FAKE), dict(kr=FAKE), dict(n_phys=1 << 31), dict(rows=1 << 31)):
+                dict(slots=None), dict(counts=None), dict(key=at["other"]), dict(kr=at["other"]), dict(n_phys=1 << 31), dict(rows=1 << 31)):
+        assert call(**bad) == INVALID, bad
+    # outputs that share memory with an input, or with one another
+    for bad in (dict(kv=at["cached"]), dict(kv=at["new"]), dict(pos=at["slots"]), dict(tables=at["free"]), dict(ro=at["to"]), dict(pt=at["tables"]),
+                dict(kv=ctypes.c_void_p(at["cached"].value + 24)), dict(counts=ctypes.c_void_p(at["ro"].value + 32)), dict(key=at["slots"], kr=at["other"]),
+                dict(rs=ctypes.c_void_p(at["tables"].value + 4 * 63))):
         assert call(**bad) == INVALID, bad
     assert call(B=8193) == UNSUPPORTED
     assert call(B=8192, width=1 << 18, ld=1 << 18) == UNSUPPORTED      # 2^31 pages
@@ -85,10 +92,10 @@ def test_attn_decode_shared_refusals(lib):
 
     for bad in (dict(B=-1), dict(H=0), dict(H=30), dict(dqk=0), dict(n=0), dict(page=0), dict(P=-1), dict(most=999), dict(scale=0.0), dict(scale=-1.0),
                 dict(scale=math.nan), dict(scale=math.inf), dict(q=None), dict(kp=None), dict(vp=None), dict(out=None), dict(lens=None), dict(pt=None), dict(tables=None),
-                dict(off=None), dict(q=ODD), dict(kp=ODD), dict(out=ODD), dict(ws=ODD), dict(kps=32769), dict(vts=513), dict(vp=FAKE, dv=136), dict(vp=FAKE, vps=65536)):
+                dict(off=None), dict(q=ODD), dict(kp=ODD), dict(out=ODD), dict(ws=ODD), dict(kps=32769), dict(vts=513), dict(vp=FAKE, dv=136), dict(vp=FAKE, vps=65536), dict(phys=0), dict(kts=0), dict(vhs=-128), dict(kps=-32768)):
         assert call(**bad) == INVALID, bad
     assert call(dqk=132) == UNSUPPORTED and call(dqk=640) == UNSUPPORTED and call(dv=520) == UNSUPPORTED
-    assert call(most=(1 << 31) - 100) == UNSUPPORTED
+    assert call(most=(1 << 31) - 100) == UNSUPPORTED and call(B=65536, bytes=1 << 60) == UNSUPPORTED
     assert call(bytes=need - 1) == TOO_SMALL
     assert call(B=0) == 0
 
