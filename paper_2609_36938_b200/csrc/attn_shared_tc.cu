@@ -93,6 +93,14 @@ struct StShape {
     static constexpr int SMEM = Q_BYTES + SLOTS * SLOT + static_cast<int>(sizeof(StShared));
 };
 
+// A row's outputs in a segment: one from every fragment (more than 128 rows), or one from each group of every fragment.
+struct alignas(8) SmPart {
+    int n, row, step, unused;
+    int64_t place;                       // of the first, in groups; step to the next
+};
+
+constexpr int SM_ROWS = 8;      // rows of a block of the merge
+
 struct StParams {
     const uint16_t* q;
     int B, H_q, n_kv, group;
@@ -110,7 +118,7 @@ struct StParams {
     float scale_log2e;
     float *pre_o, *own_o;                // [place][2][d_v / 4][rows][4], rows: 128, chunk_rows
     float2 *pre_ml, *own_ml;             // [place][2][rows]: maximum and sum
-    int32_t* own_base;                   // for the merge
+    SmPart* places;                      // for the merge: [kv head][row, filled up to SM_ROWS][prefix, own]
     int n_ctas;
     uint16_t* out;
     float* lse;
@@ -497,13 +505,9 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
         for (int b = b0; b < b1; ++b) {
             const int n = sh->own_base[b];
             sh->own_base[b] = before;
-            if (blockIdx.x == 0) p.own_base[b] = before;
             before += n;
         }
-        if (lane == 0) {
-            sh->own_base[p.B] = own_units;
-            if (blockIdx.x == 0) p.own_base[p.B] = own_units;
-        }
+        if (lane == 0) sh->own_base[p.B] = own_units;
         __syncwarp();
         const int units = p.prefix_units + own_units * p.n_kv * p.parts, share = st_share(p, units);
         int u = min(static_cast<int64_t>(share) * cta, static_cast<int64_t>(units));
@@ -549,6 +553,37 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
                 }
                 __syncwarp();
             }
+        }
+        // Meanwhile, for the merge: where the outputs of the rows lie.  Every CTA takes some rows; a lane for a row's prefix segment, one for its own.
+        const int x_rows = p.B * p.group, blocks = (x_rows + SM_ROWS - 1) / SM_ROWS, all = blocks * SM_ROWS * p.n_kv * 2;
+        const float inv_share = __frcp_rn(static_cast<float>(share)), inv_group = __frcp_rn(static_cast<float>(p.group)), inv_rows = __frcp_rn(static_cast<float>(blocks * SM_ROWS));
+        for (int i = cta * 32 + lane; i < all; i += p.n_ctas * 32) {
+            SmPart part = {};
+            const int h = st_divide(i >> 1, blocks * SM_ROWS, inv_rows), x = (i >> 1) - h * blocks * SM_ROWS, b = st_divide(x, p.group, inv_group), g = x - b * p.group;
+            bool bad;
+            if (x < x_rows && st_length(p, b, bad) > 0) {
+                const int segments = p.n_kv * p.parts, sub = g / ST_ROWS, c = b * p.parts + sub;
+                if ((i & 1) == 0 && p.prefix > 0) {
+                    const int tile = st_divide(c, 2 * p.per_tile, __frcp_rn(static_cast<float>(2 * p.per_tile))), in_tile = c - tile * 2 * p.per_tile;
+                    const int half = in_tile >= p.per_tile ? 1 : 0, s = tile * p.n_kv + h;
+                    int w;
+                    const int u0 = st_prefix_segment(p, s, w), first = st_divide(u0, share, inv_share);
+                    part.n = st_divide(u0 + st_units(p.prefix_tiles, w) - 1, share, inv_share) - first + 1;
+                    part.place = 2 * (static_cast<int64_t>(first) + s) + half;
+                    part.step = 2;
+                    if (s >= p.heavy_segments) { part.n *= 2; part.step = 1; }
+                    part.row = (in_tile - half * p.per_tile) * p.chunk_rows + (g - sub * ST_ROWS);
+                }
+                const int base = sh->own_base[b], seg = sh->own_base[b + 1] - base;
+                if ((i & 1) != 0 && seg > 0) {
+                    const int k = h * p.parts + sub, u0 = p.prefix_units + base * segments + k * seg, first = st_divide(u0, share, inv_share);
+                    part.n = 2 * (st_divide(u0 + seg - 1, share, inv_share) - first + 1);
+                    part.place = 2 * (static_cast<int64_t>(first) + static_cast<int64_t>(b) * segments + k);
+                    part.step = 1;
+                    part.row = g - sub * ST_ROWS;
+                }
+            }
+            p.places[i] = part;
         }
         // (what is on its way has landed before the CTA leaves, also after a wait somewhere gave up)
         for (uint32_t n = n_q > 2u ? n_q - 2u : 0u; n < n_q; ++n)
@@ -789,19 +824,18 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
 
 // ---- merge: a block takes eight rows that lie one behind the other in the segments (128 bytes of every output at a time); its threads are
 // (row, four dims, share of the row's outputs), HERE fours of dims.  A thread loads maxima, sums and outputs of AT_ONCE fragments together.
-constexpr int SM_ROWS = 8;
-
-// A row's outputs in a segment: one from every fragment (more than 128 rows), or one from each group of every fragment.
-struct SmPart {
-    int n, row, step;
-    int64_t place;                       // of the first, in groups; step to the next
-};
+__device__ __forceinline__ SmPart sm_load(const SmPart* p) {
+    SmPart s;
+    const int64_t a = ld_input(reinterpret_cast<const int64_t*>(p)), b = ld_input(reinterpret_cast<const int64_t*>(p) + 1);
+    s.n = static_cast<int>(a); s.row = static_cast<int>(a >> 32); s.step = static_cast<int>(b);
+    s.place = ld_input(reinterpret_cast<const int64_t*>(p) + 2);
+    return s;
+}
 
 template <int DV, int HERE, int SHARES, int AT_ONCE>
 __global__ void __launch_bounds__(SM_ROWS * HERE * SHARES) attn_shared_merge_kernel(const __grid_constant__ StParams p) {
     constexpr int CHUNKS = DV / 4;
     grid_launch_next();
-    __shared__ SmPart parts_s[SM_ROWS][2];
     __shared__ float2 ml_s[SHARES][SM_ROWS];
     __shared__ float4 acc_s[SHARES > 1 ? SHARES - 1 : 1][HERE][SM_ROWS];
     const int tid = threadIdx.x;
@@ -809,41 +843,8 @@ __global__ void __launch_bounds__(SM_ROWS * HERE * SHARES) attn_shared_merge_ker
     const float inv_group = __frcp_rn(static_cast<float>(p.group));
     const int x_rows = p.B * p.group, blocks = (x_rows + SM_ROWS - 1) / SM_ROWS, h = blockIdx.x / blocks, x0 = (blockIdx.x - h * blocks) * SM_ROWS;
     grid_wait();
-    // a lane for each row's segment in the prefix, one for its own
-    if (tid < 2 * SM_ROWS) {
-        SmPart part = {};
-        const int x = min(x0 + (tid >> 1), x_rows - 1), b = st_divide(x, p.group, inv_group), g = x - b * p.group;
-        // (all loads at once)
-        const int all = ld_input(p.own_base + p.B), base = ld_input(p.own_base + b), seg = ld_input(p.own_base + b + 1) - base;
-        bool bad;
-        const int64_t len = st_length(p, b, bad);
-        if (x0 + (tid >> 1) < x_rows && len > 0) {
-            const int segments = p.n_kv * p.parts, share = st_share(p, p.prefix_units + all * segments), sub = g / ST_ROWS, c = b * p.parts + sub;
-            const float inv_share = __frcp_rn(static_cast<float>(share));
-            if ((tid & 1) == 0 && p.prefix > 0) {
-                const int tile = st_divide(c, 2 * p.per_tile, __frcp_rn(static_cast<float>(2 * p.per_tile))), in_tile = c - tile * 2 * p.per_tile;
-                const int half = in_tile >= p.per_tile ? 1 : 0, s = tile * p.n_kv + h;
-                int w;
-                const int u0 = st_prefix_segment(p, s, w), cta = st_divide(u0, share, inv_share);
-                part.n = st_divide(u0 + st_units(p.prefix_tiles, w) - 1, share, inv_share) - cta + 1;
-                part.place = 2 * (static_cast<int64_t>(cta) + s) + half;
-                part.step = 2;
-                if (s >= p.heavy_segments) { part.n *= 2; part.step = 1; }
-                part.row = (in_tile - half * p.per_tile) * p.chunk_rows + (g - sub * ST_ROWS);
-            }
-            if ((tid & 1) != 0 && seg > 0) {
-                const int k = h * p.parts + sub, u0 = p.prefix_units + base * segments + k * seg, cta = st_divide(u0, share, inv_share);
-                part.n = 2 * (st_divide(u0 + seg - 1, share, inv_share) - cta + 1);
-                part.place = 2 * (static_cast<int64_t>(cta) + static_cast<int64_t>(b) * segments + k);
-                part.step = 1;
-                part.row = g - sub * ST_ROWS;
-            }
-        }
-        parts_s[tid >> 1][tid & 1] = part;
-    }
-    __syncthreads();
     const int row = tid % SM_ROWS, here = tid / SM_ROWS % HERE, chunk = blockIdx.y * HERE + here, share = tid / (SM_ROWS * HERE);
-    const SmPart pre = parts_s[row][0], own = parts_s[row][1];
+    const SmPart pre = sm_load(p.places + (static_cast<int64_t>(blockIdx.x) * SM_ROWS + row) * 2), own = sm_load(p.places + (static_cast<int64_t>(blockIdx.x) * SM_ROWS + row) * 2 + 1);
     const int n = pre.n + own.n;
     const float2* const pre_ml = p.pre_ml + pre.place * ST_ROWS + pre.row;
     const float2* const own_ml = p.own_ml + own.place * p.chunk_rows + own.row;
@@ -916,7 +917,7 @@ bool attn_shared_tc_supported(int d_qk, int d_v) { return (d_qk == 64 || d_qk ==
 struct StLayout {
     int chunk_rows, parts, per_tile;
     int64_t chunks, row_tiles, prefix_segments, pre_places, own_places;
-    size_t own_base, pre_ml, own_ml, pre_o, own_o, bytes;      // byte offsets
+    size_t merge_parts, pre_ml, own_ml, pre_o, own_o, bytes;   // byte offsets
 };
 
 static StLayout st_layout(int B, int H_q, int n_kv, int d_v, int64_t prefix, int64_t max_len) {
@@ -932,7 +933,7 @@ static StLayout st_layout(int B, int H_q, int n_kv, int d_v, int64_t prefix, int
     l.own_places = max_len > prefix ? l.chunks * n_kv + ST_MAX_CTAS : 0;
     size_t at = 0;
     auto take = [&](size_t n) { const size_t x = at; at += (n + 127) & ~static_cast<size_t>(127); return x; };
-    l.own_base = take(sizeof(int32_t) * (static_cast<size_t>(B) + 1));
+    l.merge_parts = take(2 * sizeof(SmPart) * n_kv * ((static_cast<size_t>(B) * group + SM_ROWS - 1) / SM_ROWS * SM_ROWS));
     l.pre_ml = take(sizeof(float2) * l.pre_places * 2 * ST_ROWS);
     l.own_ml = take(sizeof(float2) * l.own_places * 2 * l.chunk_rows);
     l.pre_o = take(sizeof(float) * l.pre_places * 2 * ST_ROWS * d_v);
@@ -1007,7 +1008,7 @@ static int st_launch(const SharedAttnArgs& a, StParams p, cudaStream_t stream) {
         p.B = a.B - b < at_once ? a.B - b : at_once;
         const StLayout l = st_layout(p.B, p.H_q, p.n_kv, DV, p.prefix, p.max_len);
         unsigned char* ws = static_cast<unsigned char*>(a.ws);
-        p.own_base = reinterpret_cast<int32_t*>(ws + l.own_base);
+        p.places = reinterpret_cast<SmPart*>(ws + l.merge_parts);
         p.pre_ml = reinterpret_cast<float2*>(ws + l.pre_ml);
         p.own_ml = reinterpret_cast<float2*>(ws + l.own_ml);
         p.pre_o = reinterpret_cast<float*>(ws + l.pre_o);
