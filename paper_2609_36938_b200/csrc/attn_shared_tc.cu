@@ -3,26 +3,36 @@
 //
 //     out[b,h,:] = sum_s softmax_s(scale <q[b,h,:], K_s>) V_s     over the P shared tokens and session b's own ones
 //
-// Work.  Two kinds of segment, cut into tiles of KT keys:
-//   prefix   per kv head and 256 rows: the rows are (session, head of the group) pairs, B * group of them, so that a tile of the prefix is read
-//            once for 256 rows.  With 128 dims a tile is 16.8 MFLOP against 64 KB: the matrix units bound it;
-//   own      per session and kv head: the group's heads are the rows, 8 or so; a tile is read for them alone: HBM bounds it, and the rows of an
-//            MMA that stand empty cost nothing (a tile takes 1000 cycles of MMA, 2800 of an SM's share of HBM).
-// All tiles form one line, and every CTA (one per SM, persistent) takes an equal stretch of it, whatever the sessions' lengths: each part of a
-// segment within a stretch is a fragment that leaves its maximum, sum and unnormalised output in the workspace, and a second kernel merges the
-// fragments of a row.  A fragment's place is (number of the CTA) + (number of the segment), which no two share and which the
-// merge works out again from the same lengths; so there are no counters, and the result does not depend on timing.
+// Work.  The query heads of a session that share a kv head are a chunk of rows.  Two kinds of segment, cut into tiles of KT keys:
+//   prefix   per kv head and up to 256 rows, whole chunks of several sessions: a tile of the prefix is read once for all of them.  With 128 dims and 256
+//            rows a tile is 16.8 MFLOP against 64 KB and 2048 cycles of MMAs;
+//   own      per session and kv head: one chunk, eight rows or so; a tile is read for it alone: HBM bounds it, and the rows of an MMA that stand empty
+//            cost nothing (a tile takes 1000 cycles of MMAs, 2800 of an SM's share of HBM).
+// All tiles form one line, and every CTA (one per SM, persistent) takes an equal stretch of it by weight, whatever the sessions' lengths: each part
+// of a segment within a stretch is a fragment that leaves maxima, sums and unnormalised outputs in the workspace, and a second kernel merges the
+// fragments of a row.  A fragment's place is (number of the CTA) + (number of the segment), which no two share and which
+// follows from the lengths alone; so there are no counters, and the result does not depend on timing.
 //
-// A CTA: two groups of four softmax warps (thread = row), a warp that copies, a warp that issues MMAs.  S of group w lies in tensor memory columns
-// [128 w, ...), P (bf16) over it as the A operand of P . V, O of group w in [256 + 128 w, ...).  With more than 128 rows in a segment each group has 128
-// rows and both work on every tile; with fewer, both have the same rows and take the tiles in turn, each with an output of its own.  Either way
-// the MMAs of one group run while the other does its softmax.  K and V tiles come through one ring in boxes of TMA that lie within a page (the box
-// height divides page and tile); boxes of pages that are not there, or of tokens past the end, are out of the map's bounds and arrive as zeros.
-// Keys that do not count are masked by bits that the copying warp leaves; their rows of V are cleared, as 0 * NaN is not 0.
+// A CTA: two groups of four softmax warps (thread = row), and a warp each that copies K and V, issues Q . K, issues P . V, and works out fragments and
+// fetches their queries, ahead of the others.  With more than 128 rows each group has 128 of them and both work on every tile; with fewer,
+// both have the same rows and take the tiles in turn, each with an output of its own.  Where rows are so few that there are lanes for four of each (32; two
+// with tiles of 64 keys), each lane takes a slice of a tile's keys, and the lanes' outputs join through shared memory when the fragment ends.  K and V
+// tiles come through one ring, in boxes of TMA that lie within a page (the box height divides page and tile); boxes of pages that are not there, or
+// of tokens past the end, are out of the map's bounds and arrive as zeros.  Keys that do not count are masked by bits that the copying warp leaves; their
+// rows of V are cleared, as 0 * NaN is not 0.
 //
 // The running maximum moves only when a tile exceeds it by more than 2^8, so O is rescaled a handful of times per fragment.  P is rounded to
-// bf16 (half a step, 2^-8 relative, as the output itself); the row sum adds the probabilities as they were, so the log-sum-exp is exact to fp32.
-// Every wait is bounded; on a timeout the CTA reports JANUS_DEV_WAIT_TIMEOUT and leaves when its copies have landed.
+// bf16 (half a step, 2^-8 relative, as the output itself), or goes as two terms where rows are few and the matrix units wait for memory; the row sum adds the
+// probabilities as they were, so the log-sum-exp is exact to fp32.  Every wait is bounded; on a timeout the CTA reports JANUS_DEV_WAIT_TIMEOUT and
+// leaves when its copies have landed.
+//
+// What bounds it now.  More than 128 rows: 3900 cycles a tile.  Tensor memory has room for one S beside both P and both O, so the logits of a group wait until
+// the other has taken its own into registers (MMAs 512, news of them 300, the load 300, news of that 100, the issue 300-700 because the MMAs' operands take the
+// shared memory's bandwidth); softmax 2000-2700 beside it.  96 sessions x 32 heads in 4 groups over 65536 tokens: 115 us alone (900 TFLOP/s), 120-150 in a row under the
+// board's power limit.  Tiles of 80 keys, with room for two S and two P, cost the same handshakes more often: 162-174 us.  P over S, one warp for all MMAs:
+// 3865 cycles a tile; one S and one warp: 4100.  Fewer rows: HBM, at 5-6 TB/s while tiles run (96 x 4096 own tokens 4.5 TB/s over all); a fragment costs two
+// to three us besides, of which the softmax of its last tile, P . V, and the join are 2000 + 1300 + 2900 cycles.  One session of 3000 tokens: 14.5 us, of which this
+// kernel 8, mostly the latencies of lengths, pages, first tile and instructions not yet in the cache, one after the other.
 #include <type_traits>
 
 #include "attn_shared.cuh"
@@ -67,7 +77,7 @@ struct StShared {
     uint64_t p_full[2], pv_done[2];                 // P written, O rescaled; P . V done
     uint64_t q_full[2], q_empty[2];                 // queries of 128 rows are there / their place is no longer needed
     uint64_t f_full[ST_FRAGMENTS], f_empty[ST_FRAGMENTS];      // fragment worked out / taken over by the warps that work on it
-    uint64_t pv_all;                                // the fragment's last P . V is done
+    uint64_t pv_all;                                // the last P . V of a fragment of more than 128 rows is done
     uint64_t meet[2];                               // the warps of a group wait for one another
     uint64_t drain[2];
     uint32_t partial[ST_INFO];                      // whether some key of the tile does not count
@@ -126,7 +136,7 @@ struct StParams {
 };
 
 // The line counts units: so many for a tile of more than 128 rows, for one of fewer, and for what a segment costs besides its tiles.
-constexpr int ST_HEAVY = 8, ST_LIGHT = 8, ST_SEGMENT = 12;
+constexpr int ST_HEAVY = 8, ST_LIGHT = 8, ST_SEGMENT = 6;
 
 // Lanes that share the keys of a row: where rows are so few that there are lanes for `most` of each, every one takes a slice of a tile's keys, with a
 // maximum, a sum and an output of its own until the fragment ends.  Lane i holds copy i / (128 / copies), row i % (128 / copies).
@@ -393,22 +403,29 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
         // cycles for a tile of 256 rows).  What they need of one another goes by barriers.
         constexpr uint32_t idesc = umma_idesc_major(1u, ST_ROWS, KT, 0u, 0u);
         const uint32_t q_lo = umma_desc_lo(smem_u32(q_smem), 16), k_lo = umma_desc_lo(smem_u32(ring), 16);
-        uint32_t tc = 0u, n_q = 0u, n_frag = 0u, n_other[2] = {0u, 0u};       // n_other: phases of s_free (more than 128 rows) and ...
-        uint32_t n_pv[2] = {0u, 0u};                                          // ... of pv_done (fewer), by group
+        uint32_t tc = 0u, n_q = 0u, n_other[2] = {0u, 0u};       // n_other: phases of s_free (more than 128 rows), by group
+        uint32_t n_pv[2] = {0u, 0u};                             // logits so far by group, each followed by a phase of pv_done
+        uint32_t n_all = 0u, light = 0u;                         // fragments of more than 128 rows; steps of the others
+        bool was_heavy = false;
         while (ok && next_fragment()) {
             const int tiles = f.t1 - f.t0, steps = f.heavy ? 2 * tiles : tiles;
             if (tiles == 0) continue;
             // tensor memory is laid out anew: P . V of the fragment before is done
-            ok = n_frag == 0u || wait_warp(&sh->pv_all, (n_frag - 1u) & 1u);
-            ++n_frag;
-            for (int n = 0; n < steps && ok; ++n) {       // step n: group n & 1, tile n or n / 2
-                const uint32_t w = static_cast<uint32_t>(n & 1), un = 2 * (tc + static_cast<uint32_t>(f.heavy ? n >> 1 : n)), slot = un % SLOTS;
+            if (was_heavy) ok = wait_warp(&sh->pv_all, n_all++ & 1u);
+            else if (f.heavy)
+                for (int w = 0; w < 2 && ok; ++w)
+                    if (n_pv[w] > 0u) ok = wait_warp(&sh->pv_done[w], (n_pv[w] - 1u) & 1u);
+            const bool after_heavy = was_heavy;
+            was_heavy = f.heavy != 0;
+            const uint32_t turn = f.heavy ? 0u : light & 1u;      // the group that has the first tile: they take turns across fragments
+            for (int n = 0; n < steps && ok; ++n) {       // step n: group n & 1, tile n / 2; or group (n + turn) & 1, tile n
+                const uint32_t w = static_cast<uint32_t>(n + turn) & 1u, un = 2 * (tc + static_cast<uint32_t>(f.heavy ? n >> 1 : n)), slot = un % SLOTS;
                 const uint32_t use = n_q + (f.heavy ? w : 0u);
                 if (n == 0 || (f.heavy && n == 1)) ok = wait_warp(&sh->q_full[use & 1u], (use >> 1) & 1u);
                 if (ok && (!f.heavy || w == 0u)) ok = wait_warp(&sh->full[slot], (un / SLOTS) & 1u);
                 if (ok && f.heavy && n > 0) ok = wait_warp(&sh->s_free[w ^ 1u], n_other[w ^ 1u]++ & 1u);      // the other group has the logits before
-                if (ok && !f.heavy && n > 1) ok = wait_warp(&sh->pv_done[w], n_pv[w] & 1u);                   // its P lies where the logits go
-                if (!f.heavy ? n > 1 : false) ++n_pv[w];
+                if (ok && !f.heavy && !(n < 2 && after_heavy) && n_pv[w] > 0u) ok = wait_warp(&sh->pv_done[w], (n_pv[w] - 1u) & 1u);      // its P lies where the logits go
+                ++n_pv[w];
                 if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
@@ -422,14 +439,10 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
                 }
                 __syncwarp();
             }
-            // phases that no logits wait for: those of the last steps
             if (f.heavy) {
-                if (ok) ok = wait_warp(&sh->s_free[1], n_other[1]++ & 1u);
-                n_pv[0] += static_cast<uint32_t>(tiles);
-                n_pv[1] += static_cast<uint32_t>(tiles);
+                if (ok) ok = wait_warp(&sh->s_free[1], n_other[1]++ & 1u);      // (of the last step, which no logits wait for)
             } else {
-                n_pv[0] += 1u;
-                n_pv[1] += steps > 1 ? 1u : 0u;
+                light += static_cast<uint32_t>(steps);
             }
             tc += static_cast<uint32_t>(tiles);
             n_q += f.heavy ? 2u : 1u;
@@ -443,12 +456,13 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
         // ================================================================== MMA issue: outputs
         constexpr uint32_t idesc = umma_idesc_major(1u, ST_ROWS, DV, 0u, 1u);
         const uint32_t v_lo = umma_desc_lo(smem_u32(ring), KT * 128);
-        uint32_t tc = 0u, n_p[2] = {0u, 0u};
+        uint32_t tc = 0u, n_p[2] = {0u, 0u}, light = 0u;
         while (ok && next_fragment()) {
             const int tiles = f.t1 - f.t0, steps = f.heavy ? 2 * tiles : tiles;
             const bool two = st_copies(f.heavy, f.rows, C::COPIES) > 1;
+            const uint32_t turn = f.heavy ? 0u : light & 1u;
             for (int n = 0; n < steps && ok; ++n) {
-                const uint32_t w = static_cast<uint32_t>(n & 1), un = 2 * (tc + static_cast<uint32_t>(f.heavy ? n >> 1 : n)) + 1, slot = un % SLOTS;
+                const uint32_t w = static_cast<uint32_t>(n + turn) & 1u, un = 2 * (tc + static_cast<uint32_t>(f.heavy ? n >> 1 : n)) + 1, slot = un % SLOTS;
                 if (!f.heavy || w == 0u) ok = wait_warp(&sh->full[slot], (un / SLOTS) & 1u);
                 ok = ok && wait_warp(&sh->p_full[w], n_p[w]++ & 1u);
                 if (!ok) break;
@@ -462,10 +476,11 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
                         for (int i = 0; i < KT / 16; ++i) umma_bf16_ts(d, a + KT / 2 + 8 * i, b + i * (2048 >> 4), idesc, 1u);
                     if (!f.heavy || w == 1u) umma_commit(smem_u32(&sh->empty[slot]));
                     umma_commit(smem_u32(&sh->pv_done[w]));
-                    if (n + 1 == steps) umma_commit(smem_u32(&sh->pv_all));
+                    if (f.heavy && n + 1 == steps) umma_commit(smem_u32(&sh->pv_all));
                 }
                 __syncwarp();
             }
+            light += f.heavy ? 0u : static_cast<uint32_t>(tiles);
             tc += static_cast<uint32_t>(tiles);
         }
         if (!ok) {
@@ -595,14 +610,15 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
         const uint32_t w = static_cast<uint32_t>(warp) >> 2;              // group
         const int r = threadIdx.x & 127;                                  // row of the group, lane of tensor memory
         const uint32_t lane_addr = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16), o_col = lane_addr + ST_COL_O + w * 128u;
-        uint32_t tc = 0u, n_s = 0u, n_pv = 0u, n_meet = 0u;
+        uint32_t tc = 0u, n_s = 0u, n_pv = 0u, n_meet = 0u, light = 0u;
         auto meet = [&]() {
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh->meet[w]));
             return wait_warp(&sh->meet[w], n_meet++ & 1u);
         };
         while (ok && next_fragment()) {
-            const int tiles = f.t1 - f.t0, first = f.heavy ? 0 : static_cast<int>(w), step = f.heavy ? 1 : 2;
+            const int tiles = f.t1 - f.t0, first = f.heavy ? 0 : static_cast<int>((w + light) & 1u), step = f.heavy ? 1 : 2;
+            light += f.heavy ? 0u : static_cast<uint32_t>(tiles);
             const int rows = f.heavy && w == 1u ? f.rows2 : f.rows;                // of this group
             const int copies = st_copies(f.heavy, f.rows, C::COPIES), apart = ST_ROWS / copies, copy = r / apart, row = r - copy * apart;
             const bool busy = ((warp & 3) * 32) % apart < rows;           // some row of this warp counts

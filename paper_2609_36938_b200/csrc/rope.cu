@@ -6,7 +6,7 @@
 //
 // Angles.  f_i comes as turns per position in units of 2^-64, so the phase of a position is one 64-bit product: whole turns drop out of it
 // by overflow, and at any position the error is at most position * 2^-65 turns.  (An fp32 product of position and frequency is off by 0.06 rad at position
-// 10^6.)  What is left is split into a quadrant and an eighth of a turn either side, of which sinpi and cospi are taken in fp32.
+// 10^6.)  What is left is split into a quarter turn and an eighth of a turn either side, of which sine and cosine are taken in fp32.
 //
 // What bounds it: HBM; three flops per element.  A thread takes one 16-byte chunk of the head dimension (half layout: two, half the rotated
 // part apart), works out the sines and cosines of its pairs once and applies them to the same chunk of up to RP_HEADS heads of its
