@@ -50,11 +50,9 @@ constexpr int ST_MAX_SLOTS = 8;
 static_assert(ST_INFO >= ST_MAX_SLOTS / 2 + 2, "the copying warp is at most so many tiles ahead of a softmax");
 constexpr int ST_MAX_SESSIONS = 1024;               // of one launch: their tile counts lie in shared memory
 constexpr int ST_MAX_CTAS = 148;
-// Tensor memory: O of group w in columns [256 + 128 w, ...).  With more than 128 rows one S, [0, 128), and P of group w in [128 + 64 w, ...): a group
-// takes S into registers at once, so that the next logits are computed while it still works on these.  Else S of group w in [128 w, ...), and P over it.
-constexpr uint32_t ST_COL_O = 256;
-__device__ __forceinline__ uint32_t st_col_s(bool heavy, uint32_t w) { return heavy ? 0u : 128u * w; }
-__device__ __forceinline__ uint32_t st_col_p(bool heavy, uint32_t w) { return heavy ? 128u + 64u * w : 128u * w; }
+// Tensor memory: one S in columns [0, 128), P of group w in [128 + 64 w, ...), its O in [256 + 128 w, ...).  A group takes S into registers at once, so
+// that the other group's logits are computed while it still works on these.
+constexpr uint32_t ST_COL_S = 0, ST_COL_P = 128, ST_COL_O = 256;
 
 constexpr int ST_FRAGMENTS = 4;                     // fragments that are worked out ahead
 struct StFragment {
@@ -73,11 +71,10 @@ constexpr int ST_JOIN = 20;                         // floats of a lane: 16 dims
 struct StShared {
     uint64_t full[ST_MAX_SLOTS], empty[ST_MAX_SLOTS];
     uint64_t info_full[ST_INFO];
-    uint64_t s_full[2], s_free[2];                  // by group: logits complete; in registers (more than 128 rows)
+    uint64_t s_full[2], s_free[2];                  // by group: logits complete; in registers
     uint64_t p_full[2], pv_done[2];                 // P written, O rescaled; P . V done
     uint64_t q_full[2], q_empty[2];                 // queries of 128 rows are there / their place is no longer needed
     uint64_t f_full[ST_FRAGMENTS], f_empty[ST_FRAGMENTS];      // fragment worked out / taken over by the warps that work on it
-    uint64_t pv_all;                                // the last P . V of a fragment of more than 128 rows is done
     uint64_t meet[2];                               // the warps of a group wait for one another
     uint64_t drain[2];
     uint32_t partial[ST_INFO];                      // whether some key of the tile does not count
@@ -249,7 +246,6 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
         for (int w = 0; w < 2; ++w) { mbar_init(smem_u32(&sh->s_full[w]), 1); mbar_init(smem_u32(&sh->s_free[w]), 4); mbar_init(smem_u32(&sh->p_full[w]), 4); mbar_init(smem_u32(&sh->pv_done[w]), 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&sh->q_full[i]), 1); mbar_init(smem_u32(&sh->q_empty[i]), 1); mbar_init(smem_u32(&sh->meet[i]), 4); mbar_init(smem_u32(&sh->drain[i]), 1); }
         for (int i = 0; i < ST_FRAGMENTS; ++i) { mbar_init(smem_u32(&sh->f_full[i]), 1); mbar_init(smem_u32(&sh->f_empty[i]), ST_READERS); }
-        mbar_init(smem_u32(&sh->pv_all), 1);
         fence_mbar_init();
         prefetch_tensormap(&tmap_k);
         prefetch_tensormap(&tmap_v);
@@ -403,33 +399,23 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
         // cycles for a tile of 256 rows).  What they need of one another goes by barriers.
         constexpr uint32_t idesc = umma_idesc_major(1u, ST_ROWS, KT, 0u, 0u);
         const uint32_t q_lo = umma_desc_lo(smem_u32(q_smem), 16), k_lo = umma_desc_lo(smem_u32(ring), 16);
-        uint32_t tc = 0u, n_q = 0u, n_other[2] = {0u, 0u};       // n_other: phases of s_free (more than 128 rows), by group
-        uint32_t n_pv[2] = {0u, 0u};                             // logits so far by group, each followed by a phase of pv_done
-        uint32_t n_all = 0u, light = 0u;                         // fragments of more than 128 rows; steps of the others
-        bool was_heavy = false;
+        uint32_t tc = 0u, n_q = 0u, n_free[2] = {0u, 0u}, light = 0u;       // phases of s_free by group; steps of fragments of 128 rows at most
+        int before = -1;                                                    // group of the step before
         while (ok && next_fragment()) {
             const int tiles = f.t1 - f.t0, steps = f.heavy ? 2 * tiles : tiles;
             if (tiles == 0) continue;
-            // tensor memory is laid out anew: P . V of the fragment before is done
-            if (was_heavy) ok = wait_warp(&sh->pv_all, n_all++ & 1u);
-            else if (f.heavy)
-                for (int w = 0; w < 2 && ok; ++w)
-                    if (n_pv[w] > 0u) ok = wait_warp(&sh->pv_done[w], (n_pv[w] - 1u) & 1u);
-            const bool after_heavy = was_heavy;
-            was_heavy = f.heavy != 0;
             const uint32_t turn = f.heavy ? 0u : light & 1u;      // the group that has the first tile: they take turns across fragments
             for (int n = 0; n < steps && ok; ++n) {       // step n: group n & 1, tile n / 2; or group (n + turn) & 1, tile n
                 const uint32_t w = static_cast<uint32_t>(n + turn) & 1u, un = 2 * (tc + static_cast<uint32_t>(f.heavy ? n >> 1 : n)), slot = un % SLOTS;
                 const uint32_t use = n_q + (f.heavy ? w : 0u);
                 if (n == 0 || (f.heavy && n == 1)) ok = wait_warp(&sh->q_full[use & 1u], (use >> 1) & 1u);
                 if (ok && (!f.heavy || w == 0u)) ok = wait_warp(&sh->full[slot], (un / SLOTS) & 1u);
-                if (ok && f.heavy && n > 0) ok = wait_warp(&sh->s_free[w ^ 1u], n_other[w ^ 1u]++ & 1u);      // the other group has the logits before
-                if (ok && !f.heavy && !(n < 2 && after_heavy) && n_pv[w] > 0u) ok = wait_warp(&sh->pv_done[w], (n_pv[w] - 1u) & 1u);      // its P lies where the logits go
-                ++n_pv[w];
+                if (ok && before >= 0) ok = wait_warp(&sh->s_free[before], n_free[before]++ & 1u);      // the logits before are in registers
+                before = static_cast<int>(w);
                 if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
-                    const uint32_t a = q_lo + (use & 1u) * (C::QA * ST_ROWS * 128 >> 4), b = k_lo + slot * (C::SLOT >> 4), d = tmem + st_col_s(f.heavy, w);
+                    const uint32_t a = q_lo + (use & 1u) * (C::QA * ST_ROWS * 128 >> 4), b = k_lo + slot * (C::SLOT >> 4), d = tmem + ST_COL_S;
 #pragma unroll
                     for (int i = 0; i < DQK / 16; ++i)
                         umma_bf16_ss(d, a + (i >> 2) * (ST_ROWS * 128 >> 4) + (i & 3) * 2, b + (i >> 2) * (KT * 128 >> 4) + (i & 3) * 2, idesc, i > 0 ? 1u : 0u);
@@ -439,11 +425,7 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
                 }
                 __syncwarp();
             }
-            if (f.heavy) {
-                if (ok) ok = wait_warp(&sh->s_free[1], n_other[1]++ & 1u);      // (of the last step, which no logits wait for)
-            } else {
-                light += static_cast<uint32_t>(steps);
-            }
+            light += f.heavy ? 0u : static_cast<uint32_t>(steps);
             tc += static_cast<uint32_t>(tiles);
             n_q += f.heavy ? 2u : 1u;
         }
@@ -459,7 +441,6 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
         uint32_t tc = 0u, n_p[2] = {0u, 0u}, light = 0u;
         while (ok && next_fragment()) {
             const int tiles = f.t1 - f.t0, steps = f.heavy ? 2 * tiles : tiles;
-            const bool two = st_copies(f.heavy, f.rows, C::COPIES) > 1;
             const uint32_t turn = f.heavy ? 0u : light & 1u;
             for (int n = 0; n < steps && ok; ++n) {
                 const uint32_t w = static_cast<uint32_t>(n + turn) & 1u, un = 2 * (tc + static_cast<uint32_t>(f.heavy ? n >> 1 : n)) + 1, slot = un % SLOTS;
@@ -468,15 +449,11 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
                 if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
-                    const uint32_t b = v_lo + slot * (C::SLOT >> 4), a = tmem + st_col_p(f.heavy, w), d = tmem + ST_COL_O + w * 128u;
+                    const uint32_t b = v_lo + slot * (C::SLOT >> 4), a = tmem + ST_COL_P + w * 64u, d = tmem + ST_COL_O + w * 128u;
 #pragma unroll
                     for (int i = 0; i < KT / 16; ++i) umma_bf16_ts(d, a + 8 * i, b + i * (2048 >> 4), idesc, n > 1 || i > 0 ? 1u : 0u);
-                    if (two)
-#pragma unroll
-                        for (int i = 0; i < KT / 16; ++i) umma_bf16_ts(d, a + KT / 2 + 8 * i, b + i * (2048 >> 4), idesc, 1u);
                     if (!f.heavy || w == 1u) umma_commit(smem_u32(&sh->empty[slot]));
                     umma_commit(smem_u32(&sh->pv_done[w]));
-                    if (f.heavy && n + 1 == steps) umma_commit(smem_u32(&sh->pv_all));
                 }
                 __syncwarp();
             }
@@ -622,24 +599,20 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
             const int rows = f.heavy && w == 1u ? f.rows2 : f.rows;                // of this group
             const int copies = st_copies(f.heavy, f.rows, C::COPIES), apart = ST_ROWS / copies, copy = r / apart, row = r - copy * apart;
             const bool busy = ((warp & 3) * 32) % apart < rows;           // some row of this warp counts
-            const uint32_t s_col = lane_addr + st_col_s(f.heavy, w), p_col = lane_addr + st_col_p(f.heavy, w);
+            const uint32_t s_col = lane_addr + ST_COL_S, p_col = lane_addr + ST_COL_P + w * 64u;
             float m_ref = neg_inf, l_sum = 0.f;                           // reference maximum (scaled, log2) and sum of this lane
-            // One tile.  N: lanes that share a row's keys; this one has KT / N of them.  With more than one, P goes as two terms, 16 bits of it (the matrix
-            // units wait for memory where rows are few); the first is cut off a little below p, so that both are above zero wherever p is, and an infinite value
-            // stays what it is.
+            // One tile.  N: lanes that share a row's keys; this one has KT / N of them.  P is rounded to bf16, half a step (a second term costs
+            // 512 cycles of MMAs a tile and the room for P beside S: 10 % of the time of own tokens).
             auto softmax = [&](auto copies_, bool first_tile, uint32_t info) {
                 constexpr int N = decltype(copies_)::value, KEYS = KT / N, CHUNKS = KEYS / 32, COLS = KEYS / 2;
-                constexpr bool TWO = N > 1;
                 uint32_t x[CHUNKS][32];
 #pragma unroll
                 for (int c = 0; c < CHUNKS; ++c) tmem_ld32_issue(s_col + copy * KEYS + 32 * c, x[c]);
 #pragma unroll
                 for (int c = 0; c < CHUNKS; ++c) tmem_ld_wait(x[c]);
-                if (f.heavy) {      // the logits are in registers: the other group's may be computed
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(smem_u32(&sh->s_free[w]));
-                }
+                tc_fence_before();  // the logits are in registers: the next may be computed
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh->s_free[w]));
                 if (sh->partial[info] != 0u) {
 #pragma unroll
                     for (int c = 0; c < CHUNKS; ++c) {
@@ -668,19 +641,13 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
                 constexpr int ST = COLS < 32 ? COLS : 32;                 // columns of a store
 #pragma unroll
                 for (int c = 0; c < COLS / ST; ++c) {
-                    uint32_t pk[ST], rest[TWO ? ST : 16];
+                    uint32_t pk[ST];
 #pragma unroll
                     for (int j = 0; j < ST; ++j) {
                         const int k = 2 * (c * ST + j);
                         const float2 e = ffma2(make_float2(__uint_as_float(x[k >> 5][k & 31]), __uint_as_float(x[k >> 5][(k & 31) + 1])), sc2, nm2);
                         const float2 pr = make_float2(st_exp2(e.x), st_exp2(e.y));
-                        if constexpr (TWO) {
-                            const uint32_t lo = __float_as_uint(pr.x * 0.998f), hi = __float_as_uint(pr.y * 0.998f);
-                            pk[j] = __byte_perm(lo, hi, 0x7632);
-                            rest[j] = st_pack_bf16x2(pr.x - __uint_as_float(lo & 0xffff0000u), pr.y - __uint_as_float(hi & 0xffff0000u));
-                        } else {
-                            pk[j] = st_pack_bf16x2(pr.x, pr.y);
-                        }
+                        pk[j] = st_pack_bf16x2(pr.x, pr.y);
                         sum[j & 3] = fadd2(sum[j & 3], pr);
                     }
                     if (c == 0) {
@@ -700,7 +667,6 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
                         }
                     }
                     tmem_st_issue(p_col + copy * COLS + ST * c, pk);
-                    if constexpr (TWO) tmem_st_issue(p_col + KT / 2 + copy * COLS + ST * c, rest);
                 }
                 if constexpr (N > 1) {
                     // The keys of the other copies do not count for this lane: 2^-126 of each, as 0 would make NaN of an infinite value.
@@ -708,10 +674,7 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
 #pragma unroll
                     for (int j = 0; j < COLS; ++j) zero[j] = 0x00800080u;
 #pragma unroll
-                    for (int i = 1; i < N; ++i) {
-                        tmem_st_issue(p_col + ((copy + i) & (N - 1)) * COLS, zero);
-                        if constexpr (TWO) tmem_st_issue(p_col + KT / 2 + ((copy + i) & (N - 1)) * COLS, zero);
-                    }
+                    for (int i = 1; i < N; ++i) tmem_st_issue(p_col + ((copy + i) & (N - 1)) * COLS, zero);
                 }
                 tmem_st_wait();
                 const float2 s4 = fadd2(fadd2(sum[0], sum[1]), fadd2(sum[2], sum[3]));
@@ -738,7 +701,7 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
                     if (copies == 1) softmax(std::integral_constant<int, 1>{}, t == first, n);
                     else softmax(std::integral_constant<int, C::COPIES>{}, t == first, n);
                 } else {
-                    if (f.heavy && lane == 0) mbar_arrive(smem_u32(&sh->s_free[w]));
+                    if (lane == 0) mbar_arrive(smem_u32(&sh->s_free[w]));
                     if (t != first) ok = wait_warp(&sh->pv_done[w], n_pv++ & 1u);
                 }
                 if (!ok) break;
