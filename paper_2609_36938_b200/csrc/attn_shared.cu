@@ -161,7 +161,9 @@ struct SlLayout {
     size_t offsets, row_base, token_of, tables, idx, lse, out, bytes;
 };
 
-static bool sl_latent(int H_q, int d_qk, int n_kv_heads, int d_v) { return H_q == SL_HEADS && d_qk == 576 && n_kv_heads == 1 && d_v == SL_DV; }
+static bool sl_latent(int H_q, int d_qk, int n_kv_heads, int d_v, int64_t max_len) {
+    return H_q == SL_HEADS && d_qk == 576 && n_kv_heads == 1 && d_v == SL_DV && max_len > 0;
+}
 
 static SlLayout sl_layout(int B, bool latent, int page_size, int64_t prefix, int64_t max_len) {
     SlLayout l = {};
@@ -199,7 +201,7 @@ extern "C" size_t janus_attn_decode_shared_workspace_size(int B, int H_q, int d_
     using namespace janus;
     if (B <= 0 || H_q <= 0 || d_qk <= 0 || n_kv_heads <= 0 || d_v <= 0 || page_size <= 0 || prefix_len < 0 || max_len < prefix_len) return 0;
     if (attn_shared_tc_supported(d_qk, d_v)) return attn_shared_tc_workspace(B, H_q, n_kv_heads, d_v, prefix_len, max_len);
-    return sl_layout(B, sl_latent(H_q, d_qk, n_kv_heads, d_v), page_size, prefix_len, max_len).bytes;
+    return sl_layout(B, sl_latent(H_q, d_qk, n_kv_heads, d_v, max_len), page_size, prefix_len, max_len).bytes;
 }
 
 extern "C" int janus_attn_decode_shared(const void* q, int B, int H_q, int d_qk, const void* k_pool, int64_t k_page_stride, int64_t k_tok_stride,
@@ -210,7 +212,7 @@ extern "C" int janus_attn_decode_shared(const void* q, int B, int H_q, int d_qk,
     using namespace janus;
     if (B < 0 || H_q <= 0 || d_qk <= 0 || d_v <= 0 || n_kv_heads <= 0 || page_size <= 0 || n_phys_pages < 0 || prefix_len < 0 || max_len < prefix_len)
         return JANUS_ERR_INVALID_ARG;
-    if (H_q % n_kv_heads != 0 || !(softmax_scale > 0.f) || softmax_scale > 3.4e38f) return JANUS_ERR_INVALID_ARG;
+    if (H_q % n_kv_heads != 0 || !(softmax_scale > 0.f) || softmax_scale > 2.3e38f) return JANUS_ERR_INVALID_ARG;
     if ((d_qk % 8) != 0 || (d_v % 8) != 0 || d_qk > 576 || d_v > 512) return JANUS_ERR_UNSUPPORTED;
     if (n_phys_pages > INT32_MAX || page_size > (1 << 30) || max_len > INT32_MAX - 2 * static_cast<int64_t>(page_size)) return JANUS_ERR_UNSUPPORTED;
     if (B == 0) return JANUS_OK;
@@ -233,7 +235,7 @@ extern "C" int janus_attn_decode_shared(const void* q, int B, int H_q, int d_qk,
                                       dev_status}, stream);
 
     // (the two kernels of this route: the latent one takes aliased values alone)
-    const bool latent = sl_latent(H_q, d_qk, n_kv_heads, d_v) && max_len > 0 &&
+    const bool latent = sl_latent(H_q, d_qk, n_kv_heads, d_v, max_len) &&
                         sparse_attn_latent_tc_supported(B, H_q, d_qk, k_pool, v_pool, k_page_stride, k_tok_stride, n_kv_heads, d_v, 256);
     const SlLayout l = sl_layout(B, latent, page_size, prefix_len, max_len);
     if (l.rows > (1 << 30) / SL_HEADS || l.pieces > 0x7fffffff || l.width > INT32_MAX) return JANUS_ERR_UNSUPPORTED;

@@ -226,7 +226,7 @@ static int rp_launch(RpParams& p, bool wide, cudaStream_t stream) {
         j.inv_row = static_cast<uint32_t>(std::min<uint64_t>((1ull << 32) / (static_cast<uint64_t>(j.groups) * j.chunks), UINT32_MAX));
         j.inv_chunks = static_cast<uint32_t>(std::min<uint64_t>((1ull << 32) / j.chunks, UINT32_MAX));
         blocks += (static_cast<uint64_t>(p.T) * j.groups * j.chunks + RP_THREADS - 1) / RP_THREADS;
-        if (blocks > 0x7fffffffu) return JANUS_ERR_UNSUPPORTED;
+        if (blocks > 0x7fffffffu || static_cast<int64_t>(j.groups) * j.chunks > INT32_MAX) return JANUS_ERR_UNSUPPORTED;
     }
     if (blocks == 0) return JANUS_OK;
     const dim3 grid(static_cast<unsigned>(blocks));
@@ -265,6 +265,7 @@ extern "C" int janus_rope(const void* x, int64_t x_row_stride, int64_t x_head_st
     using namespace janus;
     if (T < 0 || H < 0 || D <= 0 || rot_offset < 0 || rot_dim <= 0 || (rot_dim & 1) || rot_offset > D - rot_dim) return JANUS_ERR_INVALID_ARG;
     if (dtype != JANUS_ELEM_BF16 && dtype != JANUS_ELEM_FP16 && dtype != JANUS_ELEM_FP32) return JANUS_ERR_UNSUPPORTED;
+    if (D > (1 << 28)) return JANUS_ERR_UNSUPPORTED;
     if (T == 0 || H == 0) return JANUS_OK;
     if (!x || !out || !positions || !freqs) return JANUS_ERR_INVALID_ARG;
     const int elem = dtype == JANUS_ELEM_FP32 ? 4 : 2;
@@ -299,6 +300,7 @@ extern "C" int janus_rope_append(const void* q, int64_t q_row_stride, int64_t q_
     if (has_q && H_q <= 0) return JANUS_ERR_INVALID_ARG;
     if (has_v && d_v <= 0) return JANUS_ERR_INVALID_ARG;
     if ((d_qk % 8) != 0 || (has_v && (d_v % 8) != 0)) return JANUS_ERR_UNSUPPORTED;
+    if (d_qk > (1 << 28) || (has_v && d_v > (1 << 28))) return JANUS_ERR_UNSUPPORTED;
     if (T == 0) return JANUS_OK;
     if (!k || !k_pool || !positions || !slots || !freqs || (has_q && (!q || !q_out)) || (has_v && (!v || !v_pool))) return JANUS_ERR_INVALID_ARG;
     if (has_v && v_pool == k_pool) return JANUS_ERR_INVALID_ARG;                     // two rows for one place

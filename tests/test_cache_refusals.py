@@ -103,6 +103,8 @@ def test_attn_decode_shared_refusals(lib):
 def test_workspace_of_nothing_is_nothing(lib):
     assert lib.janus_attn_decode_shared_workspace_size(0, 32, 128, 4, 128, 64, 1000, 3000) == 0
     assert lib.janus_attn_decode_shared_workspace_size(4, 32, 128, 4, 128, 64, 1000, 999) == 0
+    # latent sessions that are all empty go by the general route, which keeps an offset for each
+    assert lib.janus_attn_decode_shared_workspace_size(1000, 128, 576, 1, 512, 64, 0, 0) >= 8 * 1001
 
 
 def test_binding_refuses(lib):

@@ -127,6 +127,19 @@ def test_more_sessions_than_a_launch_takes():
     B.check_dev_status()
 
 
+@pytest.mark.parametrize("layout", ["gqa", "latent", "odd"])
+def test_a_batch_that_stands_empty(layout):
+    """No session has a token and none can have one: zeros and -inf, and nothing is written behind the workspace."""
+    hq, n, dqk, dv, _ = LAYOUTS[layout]
+    c = make(8, layout, np.full(700, 3), 0, 16)
+    c["lens"].zero_()
+    need = B.attn_decode_shared_workspace_size(700, hq, dqk, n, dv, 16, 0, 0)
+    buf = torch.full((need + 65536,), 7, dtype=torch.uint8, device="cuda")
+    out, lse = call(c, max_len=0, workspace=buf[:need], want_lse=True)
+    torch.cuda.synchronize()
+    assert (out == 0).all() and (lse == -math.inf).all() and (buf[need:] == 7).all()
+
+
 def test_lengths_far_below_their_bound():
     """max_len is a bound only: a bound of 2^20 tokens over short sessions changes no bit of a row's sums beyond their order."""
     for layout in ("gqa", "latent"):
