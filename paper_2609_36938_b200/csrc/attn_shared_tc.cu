@@ -25,15 +25,15 @@
 // bf16 (half a step, 2^-8 relative, as the output itself); the row sum adds the probabilities as they were, so the log-sum-exp is exact to fp32.  Every
 // wait is bounded; on a timeout the CTA reports JANUS_DEV_WAIT_TIMEOUT and leaves when its copies have landed.
 //
-// What bounds it now.  More than 128 rows: 3900 cycles a tile.  Tensor memory has room for one S beside both P and both O, so the logits of a group wait until
-// the other has taken its own into registers (MMAs 512, news of them 300, the load 300, news of that 100, the issue 300-700 because the MMAs' operands take the
-// shared memory's bandwidth); softmax 2000-2700 beside it.  96 sessions x 32 heads in 4 groups over 65536 tokens: 116 us (890 TFLOP/s), 130 in a row of
-// thousands, as the power limit takes the clock from 1965 to some 1850 MHz.  Tiles of 80 keys, with room for two S and two P, cost the same handshakes more
-// often: 162-174 us.  P over S, one warp for all MMAs: 3865 cycles a tile; one S and one warp: 4100.  Fewer rows: HBM, 6.0 TB/s while tiles run (96 sessions'
-// own tokens from 2048 to 4096: 67 us for 403 MB; P over S, an S for each group: 5.3), less with small pages, as a box costs the copying some 100 cycles
-// (8192 own tokens of 37 sessions, 8 heads of their own: pages of 64 226 us, of 16 314, of 8 445).  A fragment costs two to three us besides: the softmax of
-// its last tile, P . V and the join are 1400 + 1000 + 2900 cycles.  One session of 3000 tokens: 14 us, of which this kernel 8, mostly the latencies of
-// lengths, pages, first tile and instructions not yet in the cache, one after the other.
+// What bounds it now.  More than 128 rows: 4100 cycles a tile.  Tensor memory has room for one S beside both P and both O, so the logits of a group wait until
+// the other has taken its own into registers (MMAs 900, as P . V of the other group runs between them, news of them 450, the load and news of that 660);
+// softmax 2400 beside it.  96 sessions x 32 heads in 4 groups over 65536 tokens: 116 us (890 TFLOP/s), 130 in a row of thousands, as the power limit takes the
+// clock from 1965 to some 1850 MHz.  Tiles of 80 keys, with room for two S and two P, cost the same handshakes more often: 162-174 us.  Logits handed over 64
+// keys at a time, half of S computed while the other half is read: 116 us too, as an MMA of half the keys reads all of Q again.  One warp for all MMAs: no less.
+// Fewer rows: HBM, 6.0 TB/s while tiles run (96 sessions' own tokens from 2048 to 4096: 67 us for 403 MB; P over S, an S for each group: 5.3), less with
+// small pages, as a box costs the copying some 100 cycles (8192 own tokens of 37 sessions, 8 heads of their own: pages of 64 226 us, of 16 314, of 8 445).
+// A fragment costs two to three us besides: the softmax of its last tile, P . V and the join are 1400 + 1000 + 2900 cycles.  One session of 3000 tokens: 14 us,
+// of which this kernel 8, mostly the latencies of lengths, pages, first tile and instructions not yet in the cache, one after the other.
 #include <type_traits>
 
 #include "attn_shared.cuh"
