@@ -671,7 +671,7 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
                 }
                 if constexpr (N > 1) {
                     // The keys of the other copies do not count for this lane: 2^-126 of each, as 0 would make NaN of an infinite value (of finite
-                    // values up to 3.4e38 at most 4 a key in all, beside a weight of 1 for the largest).
+                    // values up to 3.4e38 at most 4 a key, beside a weight of 1 for the largest).
                     uint32_t zero[COLS];
 #pragma unroll
                     for (int j = 0; j < COLS; ++j) zero[j] = 0x00800080u;
