@@ -432,7 +432,7 @@ int janus_rope_append(const void* q, int64_t q_row_stride, int64_t q_head_stride
  *
  * where token s < P lies in page prefix_table[s / page_size], and token s >= P in page page_tables[table_offsets[b] + s / page_size] (a
  * session's table covers it from its first token on, as janus_batch_plan makes it; the entries of the shared tokens are not read).
- * The rows of the prefix are read once for all sessions.
+ * The tensor-core kernel (below) reads the rows of the prefix once for many sessions (as many as fill 256 rows with their heads).
  *
  *   q          [B, H_q, d_qk] bf16, dense; out [B, H_q, d_v] bf16; lse [B, H_q] fp32 (log-sum-exp of the scaled logits) or NULL
  *   pools      as for janus_sparse_attn_prefill, with strides of their own for v_pool; v_pool may be k_pool, with its strides; n_phys_pages
