@@ -604,7 +604,7 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
             float m_ref = neg_inf, l_sum = 0.f;                           // reference maximum (scaled, log2) and sum of this lane
             // One tile.  N: lanes that share a row's keys; this one has KT / N of them.  P is rounded to bf16, half a step (a second term costs
             // 512 cycles of MMAs a tile and the room for P beside S: 10 % of the time of own tokens).
-            auto softmax = [&](auto copies_, bool first_tile, uint32_t info) {
+            auto softmax = [&](auto copies_, bool rested, uint32_t info) {
                 constexpr int N = decltype(copies_)::value, KEYS = KT / N, CHUNKS = KEYS / 32, COLS = KEYS / 2;
                 uint32_t x[CHUNKS][32];
 #pragma unroll
@@ -653,7 +653,7 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
                     }
                     if (c == 0) {
                         // the group's last P . V is done: its P may be overwritten, and O is at rest
-                        if (!first_tile) ok = wait_warp(&sh->pv_done[w], n_pv++ & 1u);
+                        if (!rested) ok = wait_warp(&sh->pv_done[w], n_pv++ & 1u);
                         if (!ok) return;
                         tc_fence_after();
                         if (__any_sync(0xffffffffu, moved)) {
@@ -689,8 +689,14 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
                 if (!ok) break;
                 ++n_s;
                 tc_fence_after();
+                bool rested = t == first;                                 // the group's P . V of the tile before is known to be done
                 if (sh->partial[n] != 0u) {
-                    // rows of V that do not count: zeros, once they have landed
+                    // Rows of V that do not count: zeros, once they have landed.  The slot held V of SLOTS / 2 tiles before, the group's own tile before
+                    // with four slots: its P . V is waited for first, as a barrier does not tell this V's phase from the one before that V's.  (More slots
+                    // leave tiles between; of the fragment before this one the group has waited for everything.)
+                    if (!rested) ok = wait_warp(&sh->pv_done[w], n_pv++ & 1u);
+                    if (!ok) break;
+                    rested = true;
                     const uint32_t un = 2 * tile + 1, slot = un % SLOTS;
                     ok = wait_warp(&sh->full[slot], (un / SLOTS) & 1u);
                     if (!ok) break;
@@ -700,11 +706,11 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
                     fence_proxy_async();
                 }
                 if (busy) {
-                    if (copies == 1) softmax(std::integral_constant<int, 1>{}, t == first, n);
-                    else softmax(std::integral_constant<int, C::COPIES>{}, t == first, n);
+                    if (copies == 1) softmax(std::integral_constant<int, 1>{}, rested, n);
+                    else softmax(std::integral_constant<int, C::COPIES>{}, rested, n);
                 } else {
                     if (lane == 0) mbar_arrive(smem_u32(&sh->s_free[w]));
-                    if (t != first) ok = wait_warp(&sh->pv_done[w], n_pv++ & 1u);
+                    if (!rested) ok = wait_warp(&sh->pv_done[w], n_pv++ & 1u);
                 }
                 if (!ok) break;
                 tc_fence_before();
