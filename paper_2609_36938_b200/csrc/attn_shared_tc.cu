@@ -94,8 +94,11 @@ struct StShape {
     static constexpr int Q_BYTES = 2 * ST_ROWS * DQK * 2, K_BYTES = KT * DQK * 2, V_BYTES = KT * DV * 2;
     static constexpr int SLOT = K_BYTES > V_BYTES ? K_BYTES : V_BYTES;
     static constexpr int ROOM = (227 * 1024 - static_cast<int>(sizeof(StShared)) - Q_BYTES) / SLOT;
-    static constexpr int SLOTS = ROOM < ST_MAX_SLOTS ? ROOM : ST_MAX_SLOTS;
-    static_assert(SLOTS >= 4, "K and V of a tile, and of the next");
+    // A multiple of four: K follows K in a slot, and V follows V of the group's own.  A barrier tells its phase from the one before only, so whoever waits
+    // for a tile must have seen the last one in its slot land (with five slots, which keys of 64 and values of 128 have room for, K would follow a V
+    // that the warp of Q . K never waits for).
+    static constexpr int SLOTS = (ROOM < ST_MAX_SLOTS ? ROOM : ST_MAX_SLOTS) / 4 * 4;
+    static_assert(SLOTS >= 4 && SLOTS % 4 == 0, "K and V of a tile, and of the next");
     static constexpr int Q_PLACE = Q_BYTES / 2;
     static constexpr int COPIES = KT / 32;                            // a row's keys are shared by so many lanes at most
     static constexpr int SMEM = Q_BYTES + SLOTS * SLOT + static_cast<int>(sizeof(StShared));

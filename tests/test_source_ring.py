@@ -92,3 +92,17 @@ def test_a_group_that_clears_rows_waits_for_the_tile_itself(heavy):
         for partial in range(9):
             bad = [e for e in early(slots, 9, heavy, partial, rests_before_clearing()) if e[0][0][0] == "clears"]
             assert not bad, (slots, partial, bad)
+
+
+def test_tiles_of_k_and_v_keep_their_slots():
+    """With a number of slots divisible by four K follows K and V follows V of the same group, whatever room there is."""
+    expression = re.search(r"static constexpr int SLOTS = ([^;]*);", code()).group(1)
+    most = int(re.search(r"ST_MAX_SLOTS = (\d+)", code()).group(1))
+    picked = re.fullmatch(r"\(?ROOM < ST_MAX_SLOTS \? ROOM : ST_MAX_SLOTS\)?(?: / 4 \* 4)?", expression)
+    assert picked, expression
+    for room in range(4, 16):
+        slots = min(room, most) // 4 * 4 if "/ 4 * 4" in expression else min(room, most)
+        for heavy in (False, True):
+            for partial in range(9):
+                bad = early(slots, 9, heavy, partial, rests_before_clearing())
+                assert not bad, (room, slots, partial, bad)
