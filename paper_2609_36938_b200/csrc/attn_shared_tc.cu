@@ -123,6 +123,8 @@ struct StParams {
     const int32_t* page_tables;
     const int64_t* table_offsets;
     const int64_t* kv_lens;
+    const uint16_t* v_pool;
+    int64_t v_page_stride, v_tok_stride, v_head_stride;
     int64_t prefix, own_start, max_len;  // own_start: where the tiles of the own tokens begin, prefix rounded down to a box
     int prefix_tiles, prefix_units;      // tiles of a segment, units of all segments
     int heavy_segments;                  // the first ones have more than 128 rows
@@ -673,11 +675,10 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
                     tmem_st_issue(p_col + copy * COLS + ST * c, pk);
                 }
                 if constexpr (N > 1) {
-                    // The keys of the other copies do not count for this lane: 2^-126 of each, as 0 would make NaN of an infinite value (of finite
-                    // values up to 3.4e38 at most 4 a key, beside a weight of 1 for the largest).
+                    // the keys of the other copies do not count for this lane (0 * inf is NaN: the merge sees to that)
                     uint32_t zero[COLS];
 #pragma unroll
-                    for (int j = 0; j < COLS; ++j) zero[j] = 0x00800080u;
+                    for (int j = 0; j < COLS; ++j) zero[j] = 0u;
 #pragma unroll
                     for (int i = 1; i < N; ++i) tmem_st_issue(p_col + ((copy + i) & (N - 1)) * COLS, zero);
                 }
@@ -822,6 +823,47 @@ __device__ __forceinline__ SmPart sm_load(const SmPart* p) {
     return s;
 }
 
+// Four dims of a row some of whose sums are NaN although the row's weights are numbers.  A weight of 0 in fp32 makes NaN of an infinite value: that of a key
+// of another copy, or of one far below the largest.  Every weight is positive by the definition, so the sum is infinite where the column holds infinite values of
+// one sign, and NaN where it holds both or a NaN; it stays as it is where finite values have overflowed.  Reads the column again, eight tokens at a time.
+__device__ __noinline__ float4 st_infinite_values(const StParams& p, int b, int h, int d, float4 sum) {
+    constexpr int AT_ONCE = 8;
+    bool bad;
+    const int64_t len = st_length(p, b, bad);
+    int64_t table = 0, entries = 0;
+    if (len > p.prefix) {
+        table = ld_input(p.table_offsets + b);
+        entries = table < 0 ? 0 : ld_input(p.table_offsets + b + 1) - table;
+    }
+    uint32_t seen[4] = {0u, 0u, 0u, 0u};      // 1: infinity, 2: minus infinity, 4: NaN
+    for (int64_t s0 = 0; s0 < len; s0 += AT_ONCE) {
+        int32_t id[AT_ONCE];
+        uint2 x[AT_ONCE];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const int64_t s = s0 + k, e = s / p.page_size;
+            id[k] = -1;
+            if (s < p.prefix) id[k] = ld_input(p.prefix_table + e);
+            else if (s < len && e < entries) id[k] = ld_input(p.page_tables + table + e);
+        }
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            x[k] = make_uint2(0u, 0u);
+            if (id[k] >= 0 && id[k] < p.n_phys)
+                x[k] = ld_input(reinterpret_cast<const uint2*>(p.v_pool + id[k] * p.v_page_stride + (s0 + k) % p.page_size * p.v_tok_stride + h * p.v_head_stride + d));
+        }
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t v = ((j < 2 ? x[k].x : x[k].y) >> (16 * (j & 1))) & 0xffffu;
+                if ((v & 0x7f80u) == 0x7f80u) seen[j] |= (v & 0x7fu) != 0u ? 4u : (v >> 15) != 0u ? 2u : 1u;
+            }
+    }
+    auto whole = [](float x, uint32_t found) { return x == x || found == 0u || found > 2u ? x : __int_as_float(found == 1u ? 0x7f800000 : 0xff800000); };
+    return make_float4(whole(sum.x, seen[0]), whole(sum.y, seen[1]), whole(sum.z, seen[2]), whole(sum.w, seen[3]));
+}
+
 template <int DV, int HERE, int SHARES, int AT_ONCE>
 __global__ void __launch_bounds__(SM_ROWS * HERE * SHARES) attn_shared_merge_kernel(const __grid_constant__ StParams p) {
     constexpr int CHUNKS = DV / 4;
@@ -894,8 +936,12 @@ __global__ void __launch_bounds__(SM_ROWS * HERE * SHARES) attn_shared_merge_ker
     if (share == 0 && x < x_rows) {
         const float inv = l != 0.f ? 1.f / l : 0.f;        // (a NaN is a sum)
         const int b = st_divide(x, p.group, inv_group);
+        acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
+        const bool number = acc.x == acc.x && acc.y == acc.y && acc.z == acc.z && acc.w == acc.w;
+        if (l == 0.f) acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        else if (l == l && !number) acc = st_infinite_values(p, b, h, 4 * chunk, acc);
         const int64_t out = static_cast<int64_t>(b) * p.H_q + h * p.group + (x - b * p.group);
-        *reinterpret_cast<uint2*>(p.out + out * DV + 4 * chunk) = make_uint2(st_pack_bf16x2(acc.x * inv, acc.y * inv), st_pack_bf16x2(acc.z * inv, acc.w * inv));
+        *reinterpret_cast<uint2*>(p.out + out * DV + 4 * chunk) = make_uint2(st_pack_bf16x2(acc.x, acc.y), st_pack_bf16x2(acc.z, acc.w));
         if (p.lse != nullptr && chunk == 0) p.lse[out] = l != 0.f ? ((m == neg_inf ? 0.f : m) + log2f(l)) * 0.6931471805599453f : neg_inf;
     }
 }
@@ -1038,6 +1084,8 @@ int launch_attn_shared_tc(const SharedAttnArgs& a, cudaStream_t stream) {
     }
     p.n_phys = static_cast<int>(a.n_phys_pages);
     p.prefix_table = a.prefix_table; p.page_tables = a.page_tables;
+    p.v_pool = static_cast<const uint16_t*>(a.v_pool);
+    p.v_page_stride = a.v_page_stride; p.v_tok_stride = a.v_tok_stride; p.v_head_stride = a.v_head_stride;
     p.prefix = a.prefix_len; p.max_len = a.max_len;
     p.scale_log2e = a.softmax_scale * 1.4426950408889634f;
     p.dev_status = a.dev_status;
