@@ -20,7 +20,7 @@ bool sparse_attn_latent_tc_supported(int M, int H_q, int d_qk, const void* k_poo
                                      int64_t tok_stride, int n_kv_heads, int d_v, int k);
 int launch_latent_pieces(const void* q, int n_tokens, int max_rows, const int32_t* rows, const int32_t* token_of, const void* pool, int64_t page_stride,
                          int64_t tok_stride, const int32_t* idx, int k, int page_size, const int32_t* page_tables, const int64_t* table_offsets,
-                         float softmax_scale, void* out, float* lse, int32_t* dev_status, cudaStream_t stream);
+                         float softmax_scale, float* out, float* lse, int32_t* dev_status, cudaStream_t stream);
 
 constexpr int SL_THREADS = 256;
 constexpr int SL_HEADS = 128, SL_DV = 512;      // latent layout
@@ -116,8 +116,8 @@ __global__ void __launch_bounds__(SL_THREADS) shared_list_kernel(const SlParams 
     }
 }
 
-// Output of a session from those of its pieces, and their log-sum-exps: 64 threads per head, eight dims each.
-__global__ void __launch_bounds__(SL_THREADS) shared_join_kernel(const uint16_t* piece_out, const float* piece_lse, const int32_t* row_base, uint16_t* out, float* lse) {
+// Output of a session from those of its pieces, in fp32, and their log-sum-exps: 64 threads per head, eight dims each.
+__global__ void __launch_bounds__(SL_THREADS) shared_join_kernel(const float* piece_out, const float* piece_lse, const int32_t* row_base, uint16_t* out, float* lse) {
     grid_launch_next();
     grid_wait();
     constexpr float LOG2E = 1.4426950408889634f;
@@ -132,15 +132,13 @@ __global__ void __launch_bounds__(SL_THREADS) shared_join_kernel(const uint16_t*
     for (int r = r0; r < r1; ++r) {
         const int64_t at = static_cast<int64_t>(r) * SL_HEADS + h;
         const float v = __ldcg(piece_lse + at), f = exp2f((v - safe) * LOG2E);
-        const uint4 x = __ldcg(reinterpret_cast<const uint4*>(piece_out + at * SL_DV + d));
+        const float4* src = reinterpret_cast<const float4*>(piece_out + at * SL_DV + d);
+        const float4 x = __ldcg(src), y = __ldcg(src + 1);
         if (v == neg_inf) continue;
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        const float w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
         l += f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            acc[2 * j] = fmaf(f, __uint_as_float(w[j] << 16), acc[2 * j]);
-            acc[2 * j + 1] = fmaf(f, __uint_as_float(w[j] & 0xffff0000u), acc[2 * j + 1]);
-        }
+        for (int j = 0; j < 8; ++j) acc[j] = fmaf(f, w[j], acc[j]);
     }
     const float inv = l != 0.f ? 1.f / l : 0.f;        // (a NaN is a sum)
     uint32_t w[4];
@@ -190,7 +188,7 @@ static SlLayout sl_layout(int B, bool latent, int page_size, int64_t prefix, int
     l.tables = take(sizeof(int32_t) * l.rows * l.width);
     l.idx = take(sizeof(int32_t) * l.rows * l.k);
     l.lse = take(latent ? sizeof(float) * l.rows * SL_HEADS : 0);
-    l.out = take(latent ? 2ull * l.rows * SL_HEADS * SL_DV : 0);
+    l.out = take(latent ? sizeof(float) * l.rows * SL_HEADS * SL_DV : 0);
     l.bytes = at;
     return l;
 }
@@ -257,7 +255,7 @@ extern "C" int janus_attn_decode_shared(const void* q, int B, int H_q, int d_qk,
     if (!latent)
         return launch_sparse_attn_generic(q, B, H_q, d_qk, k_pool, v_pool, k_page_stride, k_tok_stride, k_head_stride, v_page_stride, v_tok_stride, v_head_stride,
                                           n_kv_heads, d_v, p.idx, p.k, page_size, p.tables, 0, p.offsets, softmax_scale, out, lse, dev_status, stream);
-    uint16_t* piece_out = reinterpret_cast<uint16_t*>(base + l.out);
+    float* piece_out = reinterpret_cast<float*>(base + l.out);
     float* piece_lse = reinterpret_cast<float*>(base + l.lse);
     const int rc = launch_latent_pieces(q, B, static_cast<int>(l.rows), p.row_base + B, p.token_of, k_pool, k_page_stride, k_tok_stride, p.idx, p.k, page_size, p.tables,
                                         p.offsets, softmax_scale, piece_out, piece_lse, dev_status, stream);

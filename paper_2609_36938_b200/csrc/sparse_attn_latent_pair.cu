@@ -117,6 +117,7 @@ struct LpParams {
     int M;
     const int32_t* rows;            // PIECES: number of rows, at most M, and their query tokens
     const int32_t* token_of;
+    float* piece_out;               // [row][head][dim], in place of `out`
     int32_t* dev_status;
 };
 
@@ -580,13 +581,14 @@ __global__ void __launch_bounds__(LP_THREADS, 1) sparse_attn_latent_pair_kernel(
             if (lane == 0) mbar_arrive(smem_u32(x_full));
             ok = wait_warp(x_full, n_x++ & 1u);
         };
-        // output of token `it` (reference maximum m_ref): normalise, round to bf16.  Its last P.V is complete, its sums are visible.
+        // output of token `it` (reference maximum m_ref): normalise, round to bf16 (not the pieces of a token).  Its last P.V is complete, its sums are visible.
         auto write_out = [&](int it, float m_ref) {
             const float(&l)[4][LP_OWN] = sh->l[it & 1];
             const float l_sum = (l[0][h] + l[1][h]) + (l[2][h] + l[3][h]);
             const bool have_o = __any_sync(0xffffffffu, l_sum != 0.f);  // some key of one of these heads counts, be it as NaN
             const float inv = l_sum != 0.f ? 1.f / l_sum : 0.f;
-            uint16_t* orow = p.out + lp_out_offset(token(it), c, ln) + ch * 128;
+            const int64_t at = lp_out_offset(token(it), c, ln) + ch * 128;
+            uint16_t* orow = p.out + at;
             float* mo = reinterpret_cast<float*>(k_smem);               // SPLIT: nothing reads the rings any more
             if (SPLIT && part == 0) { sh->split_m[h] = m_ref; sh->split_l[h] = l_sum; }
 #pragma unroll 1
@@ -607,6 +609,14 @@ __global__ void __launch_bounds__(LP_THREADS, 1) sparse_attn_latent_pair_kernel(
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) arrive_even(&sh->o_free);
+                    }
+                    if constexpr (PIECES) {      // one of several that are still to be joined: in fp32 (on 128 bytes)
+                        float* piece = p.piece_out + at + cc * 32;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * inv);
+#pragma unroll
+                        for (int v = 0; v < 32; v += 8) st_global_v8(piece + v, o[v], o[v + 1], o[v + 2], o[v + 3], o[v + 4], o[v + 5], o[v + 6], o[v + 7]);
+                        continue;
                     }
                     uint32_t w[16];
 #pragma unroll
@@ -842,7 +852,7 @@ static int lp_resident_clusters(int dev, size_t smem, int (&n)[LP_MAX_SPLIT + 1]
 // `rows` (and `token_of`, `n_tokens`): the selection's rows are pieces of the tokens' keys (PIECES above), M of them at most; else NULL.
 static int lp_launch(const void* q, int n_tokens, int M, const void* pool, int64_t page_stride, int64_t tok_stride, const int32_t* idx, int k,
                      int page_size, const int32_t* page_table, int64_t n_logical_pages, const int64_t* table_offsets,
-                     float softmax_scale, void* out, float* lse, int32_t* dev_status, cudaStream_t stream, const int32_t* rows, const int32_t* token_of) {
+                     float softmax_scale, void* out, float* lse, int32_t* dev_status, cudaStream_t stream, const int32_t* rows, const int32_t* token_of, float* piece_out) {
     LpParams p;
     p.q = static_cast<const uint16_t*>(q);
     p.pool = static_cast<const uint16_t*>(pool);
@@ -863,7 +873,7 @@ static int lp_launch(const void* q, int n_tokens, int M, const void* pool, int64
     p.out = static_cast<uint16_t*>(out);
     p.lse = lse;
     p.M = M;
-    p.rows = rows; p.token_of = token_of;
+    p.rows = rows; p.token_of = token_of; p.piece_out = piece_out;
     p.dev_status = dev_status;
     constexpr size_t smem = LP_SMEM_TILES + 2 * LP_P_BYTES + LP_Q_BYTES + sizeof(LpShared);
     static_assert(smem <= 227 * 1024, "shared memory");
@@ -909,16 +919,16 @@ int launch_sparse_attn_latent_tc(const void* q, int M, const void* pool, int64_t
                                  int page_size, const int32_t* page_table, int64_t n_logical_pages, const int64_t* table_offsets,
                                  float softmax_scale, void* out, float* lse, int32_t* dev_status, cudaStream_t stream) {
     return lp_launch(q, M, M, pool, page_stride, tok_stride, idx, k, page_size, page_table, n_logical_pages, table_offsets, softmax_scale, out, lse, dev_status, stream,
-                     nullptr, nullptr);
+                     nullptr, nullptr, nullptr);
 }
 
-// Keys of n_tokens query tokens in pieces of k: piece r belongs to token token_of[r] and has its own page table and outputs; *rows of them (device), at
-// most max_rows.
+// Keys of n_tokens query tokens in pieces of k: piece r belongs to token token_of[r] and has its own page table, and outputs in fp32 (rounded to bf16 they would
+// leave 2^-9 of a piece in what remains of pieces that cancel); *rows of them (device), at most max_rows.
 int launch_latent_pieces(const void* q, int n_tokens, int max_rows, const int32_t* rows, const int32_t* token_of, const void* pool, int64_t page_stride,
                          int64_t tok_stride, const int32_t* idx, int k, int page_size, const int32_t* page_tables, const int64_t* table_offsets,
-                         float softmax_scale, void* out, float* lse, int32_t* dev_status, cudaStream_t stream) {
-    return lp_launch(q, n_tokens, max_rows, pool, page_stride, tok_stride, idx, k, page_size, page_tables, 0, table_offsets, softmax_scale, out, lse, dev_status, stream,
-                     rows, token_of);
+                         float softmax_scale, float* out, float* lse, int32_t* dev_status, cudaStream_t stream) {
+    return lp_launch(q, n_tokens, max_rows, pool, page_stride, tok_stride, idx, k, page_size, page_tables, 0, table_offsets, softmax_scale, nullptr, lse, dev_status, stream,
+                     rows, token_of, out);
 }
 
 }  // namespace janus
