@@ -31,10 +31,11 @@ struct SlParams {
     const int64_t* table_offsets;
     const int64_t* kv_lens;
     int64_t prefix, max_len, n_phys;
-    int B, page_size, prefix_pages, first_own, width;      // first_own: page of a session's table that holds token `prefix`
+    int B, page_size, prefix_pages, first_own, width;      // first_own: page of a session's table that holds token `prefix`; width: pages of a session
     int k, pieces;             // tokens of a row, rows of a session at most
     int32_t* idx;              // [rows, k]
-    int32_t* tables;           // [rows, width]
+    int row_width;             // table entries of a row: those of its own tokens where rows are compact
+    int32_t* tables;           // [rows, row_width]
     int64_t* offsets;          // [rows + 1]
     int32_t* row_base;         // [B + 1]: rows of the sessions before
     int32_t* token_of;         // [rows]: session of a row
@@ -75,7 +76,7 @@ __global__ void __launch_bounds__(SL_THREADS) shared_list_kernel(const SlParams 
             if (b == p.B - 1) p.row_base[p.B] = before + here;
         }
         if (piece >= here) {
-            if (b == p.B - 1 && piece == here && threadIdx.x == 0) p.offsets[row] = static_cast<int64_t>(row) * p.width;
+            if (b == p.B - 1 && piece == here && threadIdx.x == 0) p.offsets[row] = static_cast<int64_t>(row) * p.row_width;
             return;
         }
         if (threadIdx.x == 0) p.token_of[row] = b;
@@ -89,16 +90,17 @@ __global__ void __launch_bounds__(SL_THREADS) shared_list_kernel(const SlParams 
     // a page of the prefix that also holds a session's first own tokens is there twice: the tokens behind it are one page further on
     const int shift = p.prefix % p.page_size != 0 ? p.page_size : 0;
     const int64_t first = static_cast<int64_t>(piece) * p.k;
-    for (int i = threadIdx.x; i < p.k; i += SL_THREADS) {
-        const int64_t s = first + i;
-        p.idx[static_cast<int64_t>(row) * p.k + i] = s < len ? static_cast<int32_t>(s + (s < p.prefix ? 0 : shift)) : -1;
-    }
-    // the pages that the row's tokens lie in (places in its table), by one block of the session all of them where rows are not compact
+    // the pages that the row's tokens lie in, where rows are compact no others: e0 .. e1 of the session's
     const int64_t last = first + p.k < len ? first + p.k : len;
     int e0 = 0, e1 = p.width;
     if (p.compact && last > first) {
         e0 = static_cast<int>((first + (first < p.prefix ? 0 : shift)) / p.page_size);
         e1 = static_cast<int>((last - 1 + (last - 1 < p.prefix ? 0 : shift)) / p.page_size) + 1;
+    }
+    const int64_t skipped = static_cast<int64_t>(e0) * p.page_size;
+    for (int i = threadIdx.x; i < p.k; i += SL_THREADS) {
+        const int64_t s = first + i;
+        p.idx[static_cast<int64_t>(row) * p.k + i] = s < len ? static_cast<int32_t>(s + (s < p.prefix ? 0 : shift) - skipped) : -1;
     }
     for (int i = e0 + threadIdx.x; i < e1; i += SL_THREADS) {
         int32_t id = -1;
@@ -108,11 +110,11 @@ __global__ void __launch_bounds__(SL_THREADS) shared_list_kernel(const SlParams 
             const int64_t j = static_cast<int64_t>(i) - p.prefix_pages + p.first_own;
             if (j < entries) id = ld_input(p.page_tables + table + j);
         }
-        p.tables[static_cast<int64_t>(row) * p.width + i] = id < p.n_phys ? id : -1;
+        p.tables[static_cast<int64_t>(row) * p.row_width + (i - e0)] = id < p.n_phys ? id : -1;
     }
     if (threadIdx.x == 0) {
-        p.offsets[row] = static_cast<int64_t>(row) * p.width;
-        if (b == p.B - 1 && piece == p.pieces - 1) p.offsets[row + 1] = static_cast<int64_t>(row + 1) * p.width;
+        p.offsets[row] = static_cast<int64_t>(row) * p.row_width;
+        if (b == p.B - 1 && piece == p.pieces - 1) p.offsets[row + 1] = static_cast<int64_t>(row + 1) * p.row_width;
     }
 }
 
@@ -152,10 +154,12 @@ __global__ void __launch_bounds__(SL_THREADS) shared_join_kernel(const float* pi
     if (lse != nullptr && d == 0) lse[at] = l != 0.f ? safe + logf(l) : neg_inf;
 }
 
-// Lists of the route by listed tokens, and where they lie in the workspace.
+// Lists of the route by listed tokens, and where they lie in the workspace.  Sessions whose pieces could be more than SL_MOST_ROWS go so many at a time: outputs of
+// pieces take 256 KB each, 2 GB then.
+constexpr int64_t SL_MOST_ROWS = 8192;
 struct SlLayout {
-    int64_t prefix_pages, width, pieces, rows;
-    int k;
+    int64_t prefix_pages, width, row_width, pieces, rows;
+    int k, at_once;            // tokens of a row; sessions
     size_t offsets, row_base, token_of, tables, idx, lse, out, bytes;
 };
 
@@ -179,13 +183,22 @@ static SlLayout sl_layout(int B, bool latent, int page_size, int64_t prefix, int
         }
     }
     l.pieces = latent ? (max_len + l.k - 1) / l.k : 1;
-    l.rows = B * l.pieces;
+    l.at_once = B;
+    l.row_width = l.width;
+    if (latent) {
+        const int64_t most = l.pieces < SL_MOST_ROWS ? SL_MOST_ROWS / l.pieces : 1;
+        if (most < B) l.at_once = static_cast<int>(most);
+        // k consecutive tokens lie in ceil(k / page_size) + 1 pages at most, and one further where the page that the prefix ends in is there twice
+        const int64_t own = (l.k + static_cast<int64_t>(page_size) - 1) / page_size + 2;
+        if (own < l.row_width) l.row_width = own;
+    }
+    l.rows = l.at_once * l.pieces;
     size_t at = 0;
     auto take = [&](size_t n) { const size_t x = at; at += (n + 127) & ~static_cast<size_t>(127); return x; };
     l.offsets = take(sizeof(int64_t) * (l.rows + 1));
-    l.row_base = take(latent ? sizeof(int32_t) * (static_cast<size_t>(B) + 1) : 0);
+    l.row_base = take(latent ? sizeof(int32_t) * (static_cast<size_t>(l.at_once) + 1) : 0);
     l.token_of = take(latent ? sizeof(int32_t) * l.rows : 0);
-    l.tables = take(sizeof(int32_t) * l.rows * l.width);
+    l.tables = take(sizeof(int32_t) * l.rows * l.row_width);
     l.idx = take(sizeof(int32_t) * l.rows * l.k);
     l.lse = take(latent ? sizeof(float) * l.rows * SL_HEADS : 0);
     l.out = take(latent ? sizeof(float) * l.rows * SL_HEADS * SL_DV : 0);
@@ -199,7 +212,11 @@ extern "C" size_t janus_attn_decode_shared_workspace_size(int B, int H_q, int d_
     using namespace janus;
     if (B <= 0 || H_q <= 0 || d_qk <= 0 || n_kv_heads <= 0 || d_v <= 0 || page_size <= 0 || prefix_len < 0 || max_len < prefix_len) return 0;
     if (attn_shared_tc_supported(d_qk, d_v)) return attn_shared_tc_workspace(B, H_q, n_kv_heads, d_v, prefix_len, max_len);
-    return sl_layout(B, sl_latent(H_q, d_qk, n_kv_heads, d_v, max_len), page_size, prefix_len, max_len).bytes;
+    // (which of its two kernels the route takes also depends on the pools)
+    const size_t listed = sl_layout(B, false, page_size, prefix_len, max_len).bytes;
+    if (!sl_latent(H_q, d_qk, n_kv_heads, d_v, max_len)) return listed;
+    const size_t pieces = sl_layout(B, true, page_size, prefix_len, max_len).bytes;
+    return pieces > listed ? pieces : listed;
 }
 
 extern "C" int janus_attn_decode_shared(const void* q, int B, int H_q, int d_qk, const void* k_pool, int64_t k_page_stride, int64_t k_tok_stride,
@@ -243,6 +260,7 @@ extern "C" int janus_attn_decode_shared(const void* q, int B, int H_q, int d_qk,
     p.prefix = prefix_len; p.max_len = max_len; p.n_phys = n_phys_pages;
     p.B = B; p.page_size = page_size;
     p.prefix_pages = static_cast<int>(l.prefix_pages); p.first_own = static_cast<int>(prefix_len / page_size); p.width = static_cast<int>(l.width);
+    p.row_width = static_cast<int>(l.row_width);
     p.k = l.k; p.pieces = static_cast<int>(l.pieces);
     p.offsets = reinterpret_cast<int64_t*>(base + l.offsets);
     p.row_base = reinterpret_cast<int32_t*>(base + l.row_base);
@@ -251,16 +269,22 @@ extern "C" int janus_attn_decode_shared(const void* q, int B, int H_q, int d_qk,
     p.idx = reinterpret_cast<int32_t*>(base + l.idx);
     p.compact = latent;
     p.dev_status = dev_status;
-    JANUS_CUDA_CHECK(launch_kernel(shared_list_kernel, dim3(static_cast<unsigned>(l.pieces), static_cast<unsigned>(B)), SL_THREADS, 0, stream, 1, p));
-    if (!latent)
-        return launch_sparse_attn_generic(q, B, H_q, d_qk, k_pool, v_pool, k_page_stride, k_tok_stride, k_head_stride, v_page_stride, v_tok_stride, v_head_stride,
-                                          n_kv_heads, d_v, p.idx, p.k, page_size, p.tables, 0, p.offsets, softmax_scale, out, lse, dev_status, stream);
     float* piece_out = reinterpret_cast<float*>(base + l.out);
     float* piece_lse = reinterpret_cast<float*>(base + l.lse);
-    const int rc = launch_latent_pieces(q, B, static_cast<int>(l.rows), p.row_base + B, p.token_of, k_pool, k_page_stride, k_tok_stride, p.idx, p.k, page_size, p.tables,
-                                        p.offsets, softmax_scale, piece_out, piece_lse, dev_status, stream);
-    if (rc != JANUS_OK) return rc;
-    JANUS_CUDA_CHECK(launch_kernel(shared_join_kernel, dim3(SL_HEADS / (SL_THREADS / 64), static_cast<unsigned>(B)), SL_THREADS, 0, stream, 1, piece_out, piece_lse, p.row_base,
-                                   static_cast<uint16_t*>(out), lse));
+    for (int b = 0; b < B; b += l.at_once) {
+        p.B = B - b < l.at_once ? B - b : l.at_once;
+        p.kv_lens = kv_lens + b;
+        p.table_offsets = table_offsets != nullptr ? table_offsets + b : nullptr;
+        JANUS_CUDA_CHECK(launch_kernel(shared_list_kernel, dim3(static_cast<unsigned>(l.pieces), static_cast<unsigned>(p.B)), SL_THREADS, 0, stream, 1, p));
+        if (!latent)      // (all sessions at once)
+            return launch_sparse_attn_generic(q, B, H_q, d_qk, k_pool, v_pool, k_page_stride, k_tok_stride, k_head_stride, v_page_stride, v_tok_stride, v_head_stride,
+                                              n_kv_heads, d_v, p.idx, p.k, page_size, p.tables, 0, p.offsets, softmax_scale, out, lse, dev_status, stream);
+        const int64_t at = static_cast<int64_t>(b) * SL_HEADS;
+        const int rc = launch_latent_pieces(static_cast<const uint16_t*>(q) + at * d_qk, p.B, static_cast<int>(p.B * l.pieces), p.row_base + p.B, p.token_of, k_pool,
+                                            k_page_stride, k_tok_stride, p.idx, p.k, page_size, p.tables, p.offsets, softmax_scale, piece_out, piece_lse, dev_status, stream);
+        if (rc != JANUS_OK) return rc;
+        JANUS_CUDA_CHECK(launch_kernel(shared_join_kernel, dim3(SL_HEADS / (SL_THREADS / 64), static_cast<unsigned>(p.B)), SL_THREADS, 0, stream, 1, piece_out, piece_lse,
+                                       p.row_base, static_cast<uint16_t*>(out) + at * SL_DV, lse != nullptr ? lse + at : nullptr));
+    }
     return JANUS_OK;
 }

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2609_36938_b200 import binding as B
-from test_gpu_attn_shared import LAYOUTS, call, exact, make
+from test_gpu_attn_shared import LAYOUTS, call, check, exact, make
 from test_gpu_attn_shared_edges import slot
 
 pytestmark = pytest.mark.gpu
@@ -50,4 +50,42 @@ def test_infinite_entries_of_a_row(prefix, own, sign):
         if b in sees:
             fine[:, 5] = True
         assert fine.all() and ((lse[b].double() - l).abs() <= 2.0 ** -16 + 2.0 ** -20 * l.abs()).all(), b
+    B.check_dev_status()
+
+
+@pytest.mark.parametrize("page", [1, 7, 48, 192, 512])
+@pytest.mark.parametrize("prefix,own", [(515, 900), (0, 1025), (1024, 1), (255, 258)])
+def test_tables_of_pieces(prefix, own, page):
+    """A piece's table holds the pages of its own tokens, the page that the prefix ends in twice where own tokens follow in it."""
+    c = make(page, "latent", [prefix + own, prefix, prefix + own // 2], prefix, page)
+    out, lse = call(c)
+    check(c, out, lse)
+    B.check_dev_status()
+
+
+def test_more_pieces_than_are_made_at_once():
+    """300 sessions bounded by 131072 tokens: 256 of them at a time, with tables, lengths and outputs of their own."""
+    rng = torch.Generator().manual_seed(6)
+    lens = [70 + int(x) for x in torch.randint(0, 600, (300,), generator=rng)]
+    lens[3] = lens[299] = 0
+    c = make(6, "latent", lens, 70, 64)
+    need = B.attn_decode_shared_workspace_size(300, 128, 576, 1, 512, 64, 70, 131072)
+    assert need < 3 << 30
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    out, lse = call(c, max_len=131072, workspace=ws)
+    check(c, out, lse, sessions=[0, 1, 3, 100, 254, 255, 256, 257, 298, 299])
+    tight, lse2 = call(c)
+    assert (tight.float() - out.float()).abs().max() <= 2.0 ** -6 * out.float().abs().max() and torch.allclose(lse[lse > -1e30], lse2[lse > -1e30], atol=2.0 ** -14)
+    B.check_dev_status()
+
+
+def test_values_of_their_own_take_the_general_route():
+    """The latent shape with values that are no part of the keys: the other kernel, in the workspace that the same size function gives."""
+    c = make(7, "latent", [300, 260, 0, 70], 70, 16)
+    c["vp"] = c["kp"][..., :512].clone()
+    need = B.attn_decode_shared_workspace_size(4, 128, 576, 1, 512, 16, 70, 300)
+    buf = torch.full((need + 65536,), 7, dtype=torch.uint8, device="cuda")
+    out, lse = call(c, workspace=buf[:need])
+    check(c, out, lse)
+    assert (buf[need:] == 7).all()
     B.check_dev_status()
