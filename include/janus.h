@@ -360,8 +360,8 @@ int janus_sparse_attn_decode(const void* q, int B, int H_q, int d_qk,
  *   table_offsets  [B + 1] int64 out, page_tables [table_capacity] int32 out: the sessions' page tables one behind the other, as
  *                  janus_page_demand_batch, janus_sparse_attn_decode and janus_attn_decode_shared take them; entries behind the last
  *                  table are left as they were
- *   row_sessions, positions, slots   [max_rows] int32, int64, int64 out: session of a row, position c + i of its token, and its
- *                  place in the pool, page * p + position % p; rows behind the last one are written -1
+ *   row_sessions, positions, slots   [max_rows] int32, int64, int64 out: session of a row, position c + i of its token (2^63 - 1 at
+ *                  most), and its place in the pool, page * p + position % p; rows behind the last one are written -1
  *   key_rows       [max_rows] int64 out, or NULL: key_offsets[b] + position, the row of the token's indexer key where session b's keys begin
  *                  at row key_offsets[b] (given with it; -1 where slots is -1)
  *   counts         [3] int64 out: pages taken, table entries, rows; the true numbers where a capacity was exceeded

@@ -9,6 +9,7 @@
 // L2) and keeps the three exclusive sums in shared memory, then all threads of the grid go over the table entries and over the rows, each
 // finding its session by bisection of the sums (sessions differ in length by orders of magnitude; a warp per session would leave the longest
 // to one warp).  A page that is taken from the free list is known from the sums alone, so a row never reads what another thread writes.
+#include "batch_plan_rows.h"
 #include "janus_common.cuh"
 
 namespace janus {
@@ -171,14 +172,13 @@ __global__ void __launch_bounds__(BP_THREADS) batch_plan_kernel(const BpParams p
         int64_t pos = -1, slot = -1, key_row = -1;
         if (r < row_sum[p.B]) {
             const int b = bp_find(row_sum, p.B, r);
-            const int64_t c = ld_input(p.cached + b);
             session = b;
-            pos = (c > 0 ? c : 0) + (r - row_sum[b]);
-            const int64_t j = p.page_shift >= 0 ? pos >> p.page_shift : pos / p.page_size;
+            pos = bp_position(ld_input(p.cached + b), r - row_sum[b]);
+            const int32_t j = bp_page_of(pos, p.page_size, p.page_shift, page_sum[b + 1] - page_sum[b]);
             bool fresh;
-            const int32_t id = j < page_sum[b + 1] - page_sum[b] ? checked(load_page(b, static_cast<int32_t>(j), fresh)) : -1;
+            const int32_t id = j >= 0 ? checked(load_page(b, j, fresh)) : -1;
             if (id >= 0) {
-                slot = static_cast<int64_t>(id) * p.page_size + (pos - j * p.page_size);
+                slot = static_cast<int64_t>(id) * p.page_size + (pos - static_cast<int64_t>(j) * p.page_size);
                 if (p.key_rows != nullptr) key_row = ld_input(p.key_offsets + b) + pos;
             }
         }
