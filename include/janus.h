@@ -391,8 +391,8 @@ int janus_batch_plan(const int64_t* cached_lens, const int64_t* new_lens, int B,
  *   x, out      [T, H, D] bf16, fp16 or fp32 (JANUS_ELEM_*), any strides of rows and heads (in elements); out is x itself, with its
  *               strides, or memory that shares nothing with it
  *   positions   [T] int64; a negative one marks a padding row, whose part of `out` is left as it was
- *   freqs       [rot_dim / 2] uint64: f_i / (2 pi), turns per position, in units of 2^-64.  The angle of a position below 2^31 is then exact to
- *               2^-33 turns before it is rounded to fp32
+ *   freqs       [rot_dim / 2] uint64: f_i / (2 pi), turns per position, in units of 2^-64.  Before it is rounded to
+ *               fp32 an angle is off by at most 2^-33 turns, and by the position times what its entry is off by
  *   scale       factor on the rotated dims (1, or what the stretching of the frequencies asks for)
  */
 int janus_rope(const void* x, int64_t x_row_stride, int64_t x_head_stride, int64_t T, int H, int D,

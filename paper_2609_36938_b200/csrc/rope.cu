@@ -5,8 +5,8 @@
 // (pairs are neighbours, or the two halves of the rotated part; `inverse` takes -a, which is also the gradient of the forward rotation).
 //
 // Angles.  f_i comes as turns per position in units of 2^-64, so the phase of a position is one 64-bit product: whole turns drop out of it
-// by overflow, and at any position the error is at most position * 2^-65 turns.  (An fp32 product of position and frequency is off by 0.06 rad at position
-// 10^6.)  What is left is split into a quarter turn and an eighth of a turn either side, of which sine and cosine are taken in fp32.
+// by overflow, and what is left is rounded to 2^-32 turns: off by 2^-33 turns at most, beside position times what the entry is off by.  (An fp32 product
+// of position and frequency is off by 0.06 rad at position 10^6.)  It is split into a quarter turn and an eighth of a turn either side, of which sine and cosine are taken in fp32.
 //
 // What bounds it: HBM; three flops per element.  A thread takes one 16-byte chunk of the head dimension (half layout: two, half the rotated
 // part apart), works out the sines and cosines of its pairs once and applies them to the same chunk of up to RP_HEADS heads of its
@@ -56,8 +56,8 @@ struct RpParams {
     int32_t* dev_status;
 };
 
-// Sine and cosine of phase * 2^-64 turns: the nearest quarter turn is taken off, and of what is left, at most an eighth, the Taylor series: the first
-// terms left out, a^11 / 11! and a^12 / 12!, are below 2^-29.
+// Sine and cosine of phase * 2^-64 turns, to which 2^31 has been added: the high word is then the phase rounded to 2^-32 turns.  The nearest quarter turn is
+// taken off, and of what is left, at most an eighth, the Taylor series: the first terms left out, a^11 / 11! and a^12 / 12!, are below 2^-29.
 __device__ __forceinline__ void rp_turn(uint64_t phase, float& s, float& c) {
     const uint32_t top = static_cast<uint32_t>(phase >> 32), q = (top + (1u << 29)) >> 30;
     const float a = static_cast<float>(static_cast<int32_t>(top - (q << 30))) * 1.4629180792671596e-9f, b = a * a;      // 2 pi 2^-32
@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(RP_THREADS) rope_kernel(const RpParams p) {
     float s[PAIRS], c[PAIRS];
 #pragma unroll
     for (int e = 0; e < PAIRS; ++e) {
-        rp_turn(static_cast<uint64_t>(pos) * ld_input(p.freqs + chunk * PAIRS + e), s[e], c[e]);
+        rp_turn(static_cast<uint64_t>(pos) * ld_input(p.freqs + chunk * PAIRS + e) + (1ull << 31), s[e], c[e]);
         s[e] *= p.inverse ? -p.scale : p.scale;
         c[e] *= p.scale;
     }
