@@ -389,7 +389,8 @@ int janus_batch_plan(const int64_t* cached_lens, const int64_t* new_lens, int B,
  * turns by -a: what takes the gradient of y to that of x.  The other dims are copied.
  *
  *   x, out      [T, H, D] bf16, fp16 or fp32 (JANUS_ELEM_*), any strides of rows and heads (in elements); out is x itself, with its
- *               strides, or memory that shares nothing with it
+ *               strides, or memory that shares nothing with it: extents apart, or strides that show it (those of both nested, as of two slices of
+ *               one tensor); else JANUS_ERR_INVALID_ARG
  *   positions   [T] int64; a negative one marks a padding row, whose part of `out` is left as it was
  *   freqs       [rot_dim / 2] uint64: f_i / (2 pi), turns per position, in units of 2^-64.  Before it is rounded to
  *               fp32 an angle is off by at most 2^-33 turns, and by the position times what its entry is off by
@@ -404,7 +405,8 @@ int janus_rope(const void* x, int64_t x_row_stride, int64_t x_head_stride, int64
  * janus_rope_append - the new rows of a step into the paged cache: keys rotated as by janus_rope, values copied; queries, where
  * given, rotated to q_out in the same launch.  All bf16.
  *
- *   q, q_out    [T, H_q, d_qk], both NULL or both given; q_out may be q (with its strides)
+ *   q, q_out    [T, H_q, d_qk], both NULL or both given; q_out may be q (with its strides), and else shares no memory with what the call reads or
+ *               writes (as for janus_rope)
  *   k           [T, n_kv_heads, d_qk] -> k_pool, v [T, n_kv_heads, d_v] -> v_pool; v and v_pool both NULL for the latent layout, whose
  *               values are part of the key rows
  *   positions   [T] int64; slots [T] int64: row t goes to token slots[t] % page_size of page slots[t] / page_size.  Rows of slot -1
@@ -412,7 +414,7 @@ int janus_rope(const void* x, int64_t x_row_stride, int64_t x_head_stride, int64
  *               position, is skipped with JANUS_DEV_INDEX_OUT_OF_RANGE.  Slots of one call are distinct; of two rows for one slot it is not said
  *               which bytes stay.
  *   pools       strides in elements as for janus_sparse_attn_prefill, of k_pool and of v_pool each; bases and all strides on 16 bytes,
- *               d_qk and d_v multiples of 8
+ *               d_qk and d_v multiples of 8; every row of either in a place of its own.  A row of k or v that lies in a pool lies at its own slot
  */
 int janus_rope_append(const void* q, int64_t q_row_stride, int64_t q_head_stride, int H_q,
                       const void* k, int64_t k_row_stride, int64_t k_head_stride, int n_kv_heads, int d_qk,

@@ -440,7 +440,8 @@ def janus_rope(x: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, *,
                inverse: bool = False, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Rotary positions on dims [rot_offset, rot_offset + 2 len(freqs)) of every head.  x [T,H,D] bf16, fp16 or fp32 (dims of a head adjacent, other
     strides free), positions [T] int64 (negative: padding, the row of `out` stays), freqs from rope_frequencies().  interleaved: neighbouring dims are a
-    pair, else dims half the rotated part apart.  inverse: by the negative angle (the gradient).  Pass out=x to rotate in place."""
+    pair, else dims half the rotated part apart.  inverse: by the negative angle (the gradient).  Pass out=x to rotate in place; any other `out` shares no
+    memory with x.  Without `out` the padding rows of the result are undefined."""
     return _native().rope(x, positions, freqs, rot_offset, interleaved, scale, inverse, out)
 
 
@@ -449,7 +450,8 @@ def janus_rope_append(k: torch.Tensor, v: Optional[torch.Tensor], positions: tor
                       q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
     """New rows into the paged cache: keys k [T,n_kv,d_qk] rotated as by janus_rope, values v [T,n_kv,d_v] as they are, to place slots[t] (int64; page *
     page_size + token, -1: padding) of the pools [n_phys_pages, page_size, n_kv, d].  v and v_pool None: latent rows, whose values are part of the
-    keys.  q [T,H_q,d_qk] is rotated to q_out (allocated if None; q itself: in place) in the same launch; returns q_out.  All bf16."""
+    keys.  q [T,H_q,d_qk] is rotated to q_out (allocated if None, rows of negative positions undefined; q itself: in place) in the same launch; returns
+    q_out.  All bf16."""
     return _native().rope_append(k, v, positions, slots, freqs, k_pool, v_pool, rot_offset, interleaved, scale, q, q_out)
 
 

@@ -20,6 +20,7 @@
 #include <algorithm>
 
 #include "janus_common.cuh"
+#include "memory_overlap.h"
 
 namespace janus {
 
@@ -199,15 +200,9 @@ __global__ void __launch_bounds__(RP_THREADS) rope_kernel(const RpParams p) {
         }
 }
 
-// Whether no two elements of [rows, heads, dim] share memory, strides in elements.
-static bool rp_apart(int64_t rows, int64_t row_stride, int64_t heads, int64_t head_stride, int64_t dim) {
-    if (rows <= 1) row_stride = INT64_MAX / 4;
-    if (heads <= 1) head_stride = INT64_MAX / 4;
-    if (row_stride < 0 || head_stride < 0) return false;
-    const int64_t inner = row_stride < head_stride ? row_stride : head_stride, outer = row_stride < head_stride ? head_stride : row_stride;
-    const int64_t n_inner = row_stride < head_stride ? rows : heads;
-    if (inner < dim) return false;
-    return inner >= INT64_MAX / 4 || outer >= INT64_MAX / 4 || outer >= (n_inner - 1) * inner + dim;
+// [rows, heads, dim] or [pages, tokens, heads, dim], strides in elements, as it lies in memory.
+static MoTensor rp_memory(const void* at, int elem, int64_t dim, int64_t n0, int64_t stride0, int64_t n1, int64_t stride1, int64_t n2 = 1, int64_t stride2 = 0) {
+    return {reinterpret_cast<uintptr_t>(at), dim * elem, {n0, n1, n2}, {stride0 * elem, stride1 * elem, stride2 * elem}};
 }
 
 template <class T, bool NEIGHBOURS>
@@ -271,8 +266,11 @@ extern "C" int janus_rope(const void* x, int64_t x_row_stride, int64_t x_head_st
     if (!x || !out || !positions || !freqs) return JANUS_ERR_INVALID_ARG;
     const int elem = dtype == JANUS_ELEM_FP32 ? 4 : 2;
     if (((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(out)) & (elem - 1)) != 0) return JANUS_ERR_INVALID_ARG;
-    if (x_row_stride < 0 || x_head_stride < 0 || !rp_apart(T, out_row_stride, H, out_head_stride, D)) return JANUS_ERR_INVALID_ARG;
+    if (x_row_stride < 0 || x_head_stride < 0 || out_row_stride < 0 || out_head_stride < 0) return JANUS_ERR_INVALID_ARG;
+    const MoTensor out_memory = rp_memory(out, elem, D, T, out_row_stride, H, out_head_stride);
+    if (!mo_apart(out_memory)) return JANUS_ERR_INVALID_ARG;
     const bool in_place = x == out;
+    if (!in_place && mo_may_share(rp_memory(x, elem, D, T, x_row_stride, H, x_head_stride), out_memory)) return JANUS_ERR_INVALID_ARG;
     if (in_place && ((T > 1 && x_row_stride != out_row_stride) || (H > 1 && x_head_stride != out_head_stride))) return JANUS_ERR_INVALID_ARG;
     RpParams p = {};
     p.n_jobs = 1;
@@ -304,7 +302,6 @@ extern "C" int janus_rope_append(const void* q, int64_t q_row_stride, int64_t q_
     if (d_qk > (1 << 28) || (has_v && d_v > (1 << 28))) return JANUS_ERR_UNSUPPORTED;
     if (T == 0) return JANUS_OK;
     if (!k || !k_pool || !positions || !slots || !freqs || (has_q && (!q || !q_out)) || (has_v && (!v || !v_pool))) return JANUS_ERR_INVALID_ARG;
-    if (has_v && v_pool == k_pool) return JANUS_ERR_INVALID_ARG;                     // two rows for one place
     if (n_phys_pages > INT64_MAX / page_size) return JANUS_ERR_INVALID_ARG;
     RpParams p = {};
     // the longest job first: its blocks are under way before the others'
@@ -312,18 +309,28 @@ extern "C" int janus_rope_append(const void* q, int64_t q_row_stride, int64_t q_
         p.job[p.n_jobs] = rp_job(q, q_row_stride, q_head_stride, q_out, 0, T > 1 ? q_out_row_stride : 0, q_out_head_stride, T, H_q, 2);
         p.job[p.n_jobs].rotate = true;
         p.job[p.n_jobs++].head_bytes = q == q_out ? 0 : d_qk * 2;
-        if (q_row_stride < 0 || q_head_stride < 0 || !rp_apart(T, q_out_row_stride, H_q, q_out_head_stride, d_qk)) return JANUS_ERR_INVALID_ARG;
+        if (q_row_stride < 0 || q_head_stride < 0 || q_out_row_stride < 0 || q_out_head_stride < 0) return JANUS_ERR_INVALID_ARG;
         if (q == q_out && ((T > 1 && q_row_stride != q_out_row_stride) || (H_q > 1 && q_head_stride != q_out_head_stride))) return JANUS_ERR_INVALID_ARG;
     }
     if (k_row_stride < 0 || k_head_stride < 0 || k_page_stride < 0 || k_tok_stride < 0 || k_pool_head_stride < 0) return JANUS_ERR_INVALID_ARG;
-    if (!rp_apart(page_size, k_tok_stride, n_kv_heads, k_pool_head_stride, d_qk)) return JANUS_ERR_INVALID_ARG;
+    const MoTensor k_pool_memory = rp_memory(k_pool, 2, d_qk, n_phys_pages, k_page_stride, page_size, k_tok_stride, n_kv_heads, k_pool_head_stride);
+    if (!mo_apart(k_pool_memory)) return JANUS_ERR_INVALID_ARG;
+    const MoTensor q_out_memory = rp_memory(q_out, 2, d_qk, T, q_out_row_stride, has_q ? H_q : 0, q_out_head_stride);
+    if (has_q) {      // nothing that another thread still reads or also writes
+        if (!mo_apart(q_out_memory) || mo_may_share(q_out_memory, k_pool_memory)) return JANUS_ERR_INVALID_ARG;
+        if (mo_may_share(q_out_memory, rp_memory(k, 2, d_qk, T, k_row_stride, n_kv_heads, k_head_stride))) return JANUS_ERR_INVALID_ARG;
+        if (q != q_out && mo_may_share(q_out_memory, rp_memory(q, 2, d_qk, T, q_row_stride, H_q, q_head_stride))) return JANUS_ERR_INVALID_ARG;
+    }
     p.job[p.n_jobs] = rp_job(k, k_row_stride, k_head_stride, k_pool, k_page_stride, k_tok_stride, k_pool_head_stride, T, n_kv_heads, 2);
     p.job[p.n_jobs].rotate = true;
     p.job[p.n_jobs].paged = true;
     p.job[p.n_jobs++].head_bytes = d_qk * 2;
     if (has_v) {
         if (v_row_stride < 0 || v_head_stride < 0 || v_page_stride < 0 || v_tok_stride < 0 || v_pool_head_stride < 0) return JANUS_ERR_INVALID_ARG;
-        if (!rp_apart(page_size, v_tok_stride, n_kv_heads, v_pool_head_stride, d_v)) return JANUS_ERR_INVALID_ARG;
+        const MoTensor v_pool_memory = rp_memory(v_pool, 2, d_v, n_phys_pages, v_page_stride, page_size, v_tok_stride, n_kv_heads, v_pool_head_stride);
+        if (!mo_apart(v_pool_memory) || mo_may_share(k_pool_memory, v_pool_memory)) return JANUS_ERR_INVALID_ARG;      // two rows for one place
+        if (has_q && (mo_may_share(q_out_memory, v_pool_memory) || mo_may_share(q_out_memory, rp_memory(v, 2, d_v, T, v_row_stride, n_kv_heads, v_head_stride))))
+            return JANUS_ERR_INVALID_ARG;
         p.job[p.n_jobs] = rp_job(v, v_row_stride, v_head_stride, v_pool, v_page_stride, v_tok_stride, v_pool_head_stride, T, n_kv_heads, 2);
         p.job[p.n_jobs].paged = true;
         p.job[p.n_jobs++].head_bytes = d_v * 2;
