@@ -369,7 +369,8 @@ int janus_sparse_attn_decode(const void* q, int B, int H_q, int d_qk,
  * No output shares memory with an input or another output (JANUS_ERR_INVALID_ARG): a step's kv_lens may be the next step's cached_lens, which
  * then writes to other buffers.  cached_lens is what janus_page_demand_batch takes as demand_limits.  An entry of length 0 stands empty.  Where lists are too short (free
  * pages, page_tables, rows, or a session longer than width * p) the call reports JANUS_DEV_CAPACITY_EXCEEDED: a page that could not be
- * taken, and the slot of a token without a page, is -1, offsets and lengths are cut back to what is there.  A negative length counts as 0, and a
+ * taken, and the slot of a token without a page, is -1; row_offsets end at max_rows, table_offsets at table_capacity, kv_lens at width * p.  kv_lens
+ * then still counts tokens that got no row or no page: such a plan is made again, with longer lists or fewer tokens, before attention reads by it.  A negative length counts as 0, and a
  * page id outside [0, n_phys_pages) as -1, with JANUS_DEV_INDEX_OUT_OF_RANGE.  B <= 8192 and B * width < 2^31, else JANUS_ERR_UNSUPPORTED.
  */
 int janus_batch_plan(const int64_t* cached_lens, const int64_t* new_lens, int B, int page_size,
