@@ -110,7 +110,7 @@ struct alignas(8) SmPart {
     int64_t place;                       // of the first, in groups; step to the next
 };
 
-constexpr int SM_ROWS = 8;      // rows of a block of the merge
+constexpr int SM_ROWS = 8, SM_THREADS = 256;      // rows of a block of the merge, its threads
 
 struct StParams {
     const uint16_t* q;
@@ -823,11 +823,13 @@ __device__ __forceinline__ SmPart sm_load(const SmPart* p) {
     return s;
 }
 
-// Four dims of a row some of whose sums are NaN although the row's weights are numbers.  A weight of 0 in fp32 makes NaN of an infinite value: that of a key
-// of another copy, or of one far below the largest.  Every weight is positive by the definition, so the sum is infinite where the column holds infinite values of
-// one sign, and NaN where it holds both or a NaN; it stays as it is where finite values have overflowed.  Reads the column again, eight tokens at a time.
-__device__ __noinline__ float4 st_infinite_values(const StParams& p, int b, int h, int d, float4 sum) {
-    constexpr int AT_ONCE = 8;
+// Infinite values.  A weight of 0 in fp32 makes NaN of one: that of a key of another copy, or of one far below the largest.  Every weight is positive by the
+// definition, so a sum whose weights are numbers is infinite where its column holds infinite values of one sign, and NaN where it holds both or a NaN; where finite
+// values have overflowed it stays as it is.  So for rows with such a NaN the block reads its dims of the session's values again, all threads together: bits of dim d0 + i
+// in found[i]: 1 infinity, 2 minus infinity, 4 NaN.  (Here and not in the attention kernel, where other warps would wait for it.)
+template <int DIMS>
+__device__ __noinline__ void st_not_finite(const StParams& p, int b, int h, int d0, uint32_t* found) {
+    constexpr int LANES = DIMS / 8, TOKENS = SM_THREADS / LANES, AT_ONCE = 4;
     bool bad;
     const int64_t len = st_length(p, b, bad);
     int64_t table = 0, entries = 0;
@@ -835,38 +837,47 @@ __device__ __noinline__ float4 st_infinite_values(const StParams& p, int b, int 
         table = ld_input(p.table_offsets + b);
         entries = table < 0 ? 0 : ld_input(p.table_offsets + b + 1) - table;
     }
-    uint32_t seen[4] = {0u, 0u, 0u, 0u};      // 1: infinity, 2: minus infinity, 4: NaN
-    for (int64_t s0 = 0; s0 < len; s0 += AT_ONCE) {
+    const int part = threadIdx.x % LANES;
+    const uint16_t* const values = p.v_pool + h * p.v_head_stride + d0 + 8 * part;
+    uint32_t bits = 0u;      // three of each of eight dims
+    for (int64_t s0 = threadIdx.x / LANES; s0 < len; s0 += TOKENS * AT_ONCE) {
         int32_t id[AT_ONCE];
-        uint2 x[AT_ONCE];
+        uint4 x[AT_ONCE];
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
-            const int64_t s = s0 + k, e = s / p.page_size;
+            const int64_t s = s0 + k * TOKENS, e = s / p.page_size;
             id[k] = -1;
             if (s < p.prefix) id[k] = ld_input(p.prefix_table + e);
             else if (s < len && e < entries) id[k] = ld_input(p.page_tables + table + e);
         }
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
-            x[k] = make_uint2(0u, 0u);
-            if (id[k] >= 0 && id[k] < p.n_phys)
-                x[k] = ld_input(reinterpret_cast<const uint2*>(p.v_pool + id[k] * p.v_page_stride + (s0 + k) % p.page_size * p.v_tok_stride + h * p.v_head_stride + d));
+            x[k] = make_uint4(0u, 0u, 0u, 0u);
+            if (id[k] >= 0 && id[k] < p.n_phys) x[k] = ld_input(reinterpret_cast<const uint4*>(values + id[k] * p.v_page_stride + (s0 + k * TOKENS) % p.page_size * p.v_tok_stride));
         }
 #pragma unroll
-        for (int k = 0; k < AT_ONCE; ++k)
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const uint32_t w[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t v = ((j < 2 ? x[k].x : x[k].y) >> (16 * (j & 1))) & 0xffffu;
-                if ((v & 0x7f80u) == 0x7f80u) seen[j] |= (v & 0x7fu) != 0u ? 4u : (v >> 15) != 0u ? 2u : 1u;
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t v = w[j >> 1] >> (16 * (j & 1));
+                if ((v & 0x7f80u) == 0x7f80u) bits |= ((v & 0x7fu) != 0u ? 4u : (v & 0x8000u) != 0u ? 2u : 1u) << (3 * j);
             }
+        }
     }
-    auto whole = [](float x, uint32_t found) { return x == x || found == 0u || found > 2u ? x : __int_as_float(found == 1u ? 0x7f800000 : 0xff800000); };
-    return make_float4(whole(sum.x, seen[0]), whole(sum.y, seen[1]), whole(sum.z, seen[2]), whole(sum.w, seen[3]));
+    for (int j = 0; j < 8 && bits != 0u; ++j, bits >>= 3)
+        if ((bits & 7u) != 0u) atomicOr(found + 8 * part + j, bits & 7u);
+}
+// The sum in place of a NaN.
+__device__ __forceinline__ float st_not_finite_sum(float sum, uint32_t found) {
+    return sum == sum || found == 0u || found > 2u ? sum : __int_as_float(found == 1u ? 0x7f800000 : 0xff800000);
 }
 
 template <int DV, int HERE, int SHARES, int AT_ONCE>
-__global__ void __launch_bounds__(SM_ROWS * HERE * SHARES) attn_shared_merge_kernel(const __grid_constant__ StParams p) {
+__global__ void __launch_bounds__(SM_THREADS) attn_shared_merge_kernel(const __grid_constant__ StParams p) {
+    static_assert(SM_ROWS * HERE * SHARES == SM_THREADS, "a thread for every row, four dims, share");
     constexpr int CHUNKS = DV / 4;
+    __shared__ uint32_t found[HERE * 4];
     grid_launch_next();
     __shared__ float2 ml_s[SHARES][SM_ROWS];
     __shared__ float4 acc_s[SHARES > 1 ? SHARES - 1 : 1][HERE][SM_ROWS];
@@ -932,14 +943,27 @@ __global__ void __launch_bounds__(SM_ROWS * HERE * SHARES) attn_shared_merge_ker
             m = top;
         }
     }
-    const int x = x0 + row;
-    if (share == 0 && x < x_rows) {
-        const float inv = l != 0.f ? 1.f / l : 0.f;        // (a NaN is a sum)
-        const int b = st_divide(x, p.group, inv_group);
-        acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
-        const bool number = acc.x == acc.x && acc.y == acc.y && acc.z == acc.z && acc.w == acc.w;
-        if (l == 0.f) acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        else if (l == l && !number) acc = st_infinite_values(p, b, h, 4 * chunk, acc);
+    const int x = x0 + row, b = st_divide(x, p.group, inv_group);
+    const bool mine = share == 0 && x < x_rows;
+    const float inv = l != 0.f ? 1.f / l : 0.f;        // (a NaN is a sum)
+    acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
+    if (l == 0.f) acc = make_float4(0.f, 0.f, 0.f, 0.f);      // (whatever the values of keys are that have no weight)
+    const bool open = mine && l == l && (acc.x != acc.x || acc.y != acc.y || acc.z != acc.z || acc.w != acc.w);
+    if (__syncthreads_or(open))
+        for (int i = 0; i < SM_ROWS && x0 + i < x_rows; ++i) {
+            const int session = st_divide(x0 + i, p.group, inv_group);
+            if (i > 0 && session == st_divide(x0 + i - 1, p.group, inv_group)) continue;
+            if (!__syncthreads_or(open && b == session)) continue;
+            if (tid < HERE * 4) found[tid] = 0u;
+            __syncthreads();
+            st_not_finite<HERE * 4>(p, session, h, static_cast<int>(blockIdx.y) * HERE * 4, found);
+            __syncthreads();
+            if (open && b == session) {
+                acc.x = st_not_finite_sum(acc.x, found[4 * here]); acc.y = st_not_finite_sum(acc.y, found[4 * here + 1]);
+                acc.z = st_not_finite_sum(acc.z, found[4 * here + 2]); acc.w = st_not_finite_sum(acc.w, found[4 * here + 3]);
+            }
+        }
+    if (mine) {
         const int64_t out = static_cast<int64_t>(b) * p.H_q + h * p.group + (x - b * p.group);
         *reinterpret_cast<uint2*>(p.out + out * DV + 4 * chunk) = make_uint2(st_pack_bf16x2(acc.x, acc.y), st_pack_bf16x2(acc.z, acc.w));
         if (p.lse != nullptr && chunk == 0) p.lse[out] = l != 0.f ? ((m == neg_inf ? 0.f : m) + log2f(l)) * 0.6931471805599453f : neg_inf;
@@ -1067,8 +1091,8 @@ static int st_launch(const SharedAttnArgs& a, StParams p, cudaStream_t stream) {
         // Few rows have many outputs each: eight shares of them, and the dims in several blocks, as long as those are resident at once.  Many rows fill the
         // SMs with a block for eight rows.
         const int64_t blocks = (static_cast<int64_t>(p.B) * p.group + SM_ROWS - 1) / SM_ROWS * p.n_kv;
-        if (blocks * (DV / 16) <= 4 * ST_MAX_CTAS) JANUS_CUDA_CHECK(launch_kernel(attn_shared_merge_kernel<DV, 4, 8, 4>, dim3(static_cast<unsigned>(blocks), DV / 16), 256, 0, stream, 1, p));
-        else JANUS_CUDA_CHECK(launch_kernel(attn_shared_merge_kernel<DV, DV / 4, 128 / DV, 8>, dim3(static_cast<unsigned>(blocks)), 256, 0, stream, 1, p));
+        if (blocks * (DV / 16) <= 4 * ST_MAX_CTAS) JANUS_CUDA_CHECK(launch_kernel(attn_shared_merge_kernel<DV, 4, 8, 4>, dim3(static_cast<unsigned>(blocks), DV / 16), SM_THREADS, 0, stream, 1, p));
+        else JANUS_CUDA_CHECK(launch_kernel(attn_shared_merge_kernel<DV, DV / 4, 128 / DV, 8>, dim3(static_cast<unsigned>(blocks)), SM_THREADS, 0, stream, 1, p));
     }
     return JANUS_OK;
 }

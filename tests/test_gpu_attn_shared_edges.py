@@ -112,3 +112,27 @@ def test_a_row_without_a_logit_and_infinite_values(layout):
     out, lse = call(c)
     assert (out == 0).all() and (lse == -math.inf).all()
     B.check_dev_status()
+
+
+@pytest.mark.parametrize("layout,nb", [("gqa", 40), ("gqa64", 50), ("mqa200", 5), ("mha", 300), ("mha192", 140)])
+@pytest.mark.parametrize("factor", [1.0, 24.0])
+def test_infinite_values_that_all_sessions_see(layout, nb, factor):
+    """Segments of up to 256 rows, of fewer rows and of one session: infinities, a NaN and opposite infinities among the shared tokens and a session's own."""
+    prefix = 700
+    lens = [prefix + 5 * (b % 9) for b in range(nb)]
+    c = make(nb, layout, lens, prefix, 64)
+    c["kp"].mul_(factor)
+    for h, dim, s, value in ((0, 3, 0, math.inf), (0, 9, 699, -math.inf), (0, 20, 100, math.nan), (0, 33, 5, math.inf), (0, 33, 600, -math.inf), (0, 40, 300, math.inf),
+                             (0, 40, 301, math.inf)):
+        page, within = slot(c, 0, s)
+        c["vp"][page, within, h, dim] = value
+    page, within = slot(c, 8 if nb > 8 else 4, prefix + 3)
+    c["vp"][page, within, 0, 50] = -math.inf
+    out, lse = call(c)
+    for b in sorted({0, 1, 4, 8, nb // 2, nb - 1} & set(range(nb))):
+        want, _, _ = exact(c, b)
+        bad = ~torch.isfinite(want)
+        assert torch.equal(torch.isnan(out[b].double()), torch.isnan(want)) and torch.isfinite(out[b][~bad]).all(), b
+        there = bad & ~torch.isnan(want)
+        assert torch.equal(out[b].double()[there], want[there]), b
+    B.check_dev_status()
