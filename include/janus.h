@@ -451,7 +451,7 @@ int janus_rope_append(const void* q, int64_t q_row_stride, int64_t q_head_stride
  *
  * Tokens whose page is missing or outside [0, n_phys_pages) are skipped, a length below P empties its entry and one above max_len is cut back, each with
  * JANUS_DEV_INDEX_OUT_OF_RANGE.  softmax_scale > 0.  d_qk and d_v multiples of 8, d_qk <= 576, d_v <= 512, H_q a multiple of n_kv_heads; bases and strides on 16
- * bytes, strides of axes longer than one positive; B <= 65535.  A tensor-core kernel serves keys of 64, 128 or 192 dims with values of 64 or 128 in any
+ * bytes, strides of axes longer than one positive; B and H_q <= 65535.  A tensor-core kernel serves keys of 64, 128 or 192 dims with values of 64 or 128 in any
  * grouping; the latent shape (and, slowly, any other) goes through the sparse kernels with all tokens listed in the workspace.
  */
 size_t janus_attn_decode_shared_workspace_size(int B, int H_q, int d_qk, int n_kv_heads, int d_v, int page_size,

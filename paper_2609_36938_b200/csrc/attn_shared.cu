@@ -231,7 +231,7 @@ extern "C" int janus_attn_decode_shared(const void* q, int B, int H_q, int d_qk,
     if ((d_qk % 8) != 0 || (d_v % 8) != 0 || d_qk > 576 || d_v > 512) return JANUS_ERR_UNSUPPORTED;
     if (n_phys_pages > INT32_MAX || page_size > (1 << 30) || max_len > INT32_MAX - 2 * static_cast<int64_t>(page_size)) return JANUS_ERR_UNSUPPORTED;
     if (B == 0) return JANUS_OK;
-    if (B > 65535) return JANUS_ERR_UNSUPPORTED;
+    if (B > 65535 || H_q > 65535) return JANUS_ERR_UNSUPPORTED;      // (grids; fewer than 2^20 segments, as st_divide wants)
     if (!q || !k_pool || !v_pool || !out || !kv_lens) return JANUS_ERR_INVALID_ARG;
     if ((prefix_len > 0 && !prefix_table) || (max_len > prefix_len && (!page_tables || !table_offsets))) return JANUS_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(k_pool) || !aligned16(v_pool) || !aligned16(out) || !aligned16(ws)) return JANUS_ERR_INVALID_ARG;
