@@ -22,33 +22,34 @@ struct MoAxis {
     int64_t na, nb;
 };
 
-// Whether delta + sum d_i * stride_i, -na_i < d_i < nb_i, lies in (-b_bytes, a_bytes) for some d; strides descending, each no less than what the axes behind it span.
-inline bool mo_meet(const MoAxis* axes, int n, mo_int delta, mo_int a_bytes, mo_int b_bytes) {
+// Whether delta + sum d_i * stride_i, -na_i < d_i < nb_i, lies in (-b_bytes, a_bytes) for some d.  Strides descending; every d whose term the shorter strides can
+// still make up for is tried: two at most where strides are nested.  `steps`: tries left; true when they run out.
+inline bool mo_meet(const MoAxis* axes, int n, mo_int delta, mo_int a_bytes, mo_int b_bytes, int& steps) {
     if (n == 0) return -b_bytes < delta && delta < a_bytes;
+    mo_int a_inner = a_bytes, b_inner = b_bytes;                 // what one index of the first axis spans
+    for (int i = 1; i < n; ++i) {
+        a_inner += axes[i].stride * (axes[i].na - 1);
+        b_inner += axes[i].stride * (axes[i].nb - 1);
+    }
+    auto floor_div = [](mo_int x, mo_int d) { return x / d - (x % d < 0 ? 1 : 0); };
     const mo_int s = axes->stride;
-    mo_int q = -delta / s;                                       // -delta / s, rounded down
-    if (q * s > -delta) --q;
-    for (mo_int d = q; d <= q + 1; ++d)                          // any other is more than the rest can make up for
-        if (-axes->na < d && d < axes->nb && mo_meet(axes + 1, n - 1, delta + d * s, a_bytes, b_bytes)) return true;
+    mo_int first = floor_div(-b_inner - delta, s) + 1, last = floor_div(a_inner - 1 - delta, s);
+    if (first < 1 - axes->na) first = 1 - axes->na;
+    if (last > axes->nb - 1) last = axes->nb - 1;
+    for (mo_int d = first; d <= last; ++d)
+        if (--steps < 0 || mo_meet(axes + 1, n - 1, delta + d * s, a_bytes, b_bytes, steps)) return true;
     return false;
 }
 
-// False where the tensors share no byte.  True where they do, and where their extents overlap without the strides being nested (each no less than
-// what the shorter ones span, over both tensors), as then nothing is shown.
+// False where the tensors share no byte.  (True where they do, and where strides that are not nested at all leave too many combinations to try.)
 inline bool mo_may_share(const MoTensor& a, const MoTensor& b) {
     MoAxis axes[2 * MO_AXES];
     int n = 0;
-    mo_int a_extent = a.bytes, b_extent = b.bytes;
+    if (a.bytes <= 0 || b.bytes <= 0) return false;
     for (int i = 0; i < MO_AXES; ++i) {
         if (a.n[i] <= 0 || b.n[i] <= 0) return false;
-        a_extent += static_cast<mo_int>(a.n[i] - 1) * a.stride[i];
-        b_extent += static_cast<mo_int>(b.n[i] - 1) * b.stride[i];
-    }
-    if (a.bytes <= 0 || b.bytes <= 0) return false;
-    const mo_int delta = static_cast<mo_int>(b.at) - static_cast<mo_int>(a.at);
-    if (delta >= a_extent || -delta >= b_extent) return false;
-    for (int i = 0; i < MO_AXES; ++i)
         if (a.n[i] > 1 && a.stride[i] != 0) axes[n++] = {a.stride[i], a.n[i], 1};
+    }
     for (int i = 0; i < MO_AXES; ++i) {
         if (b.n[i] <= 1 || b.stride[i] == 0) continue;
         int at = 0;
@@ -57,12 +58,8 @@ inline bool mo_may_share(const MoTensor& a, const MoTensor& b) {
         else axes[at].nb = b.n[i];
     }
     std::sort(axes, axes + n, [](const MoAxis& x, const MoAxis& y) { return x.stride > y.stride; });
-    mo_int inner = a.bytes > b.bytes ? a.bytes : b.bytes;
-    for (int i = n - 1; i >= 0; --i) {
-        if (axes[i].stride < inner) return true;
-        inner += axes[i].stride * ((axes[i].na > axes[i].nb ? axes[i].na : axes[i].nb) - 1);
-    }
-    return mo_meet(axes, n, delta, a.bytes, b.bytes);
+    int steps = 1 << 16;
+    return mo_meet(axes, n, static_cast<mo_int>(b.at) - static_cast<mo_int>(a.at), a.bytes, b.bytes, steps);
 }
 
 // Whether every element has a place of its own: strides that are nested.
