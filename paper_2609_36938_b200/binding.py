@@ -366,7 +366,8 @@ def janus_batch_plan(cached_lens: torch.Tensor, new_lens: torch.Tensor, block_ta
     """Page tables, rows, positions and cache places of a step from the lengths of its sessions (int64 [B] tensors on the device).
     block_tables [B, width] int32 holds the pages of the cached tokens; the further pages come from the beginning of free_pages and are
     written behind them.  key_offsets (int64 [B] or longer): also key_rows, the places of the indexer keys.  Returns a dict of device
-    tensors; the counts stay on the device (no host sync).  ``out``: buffers from batch_plan_buffers(), none of which may be an input: a loop that
+    tensors; the counts stay on the device (no host sync).  After JANUS_DEV_CAPACITY_EXCEEDED kv_lens also counts tokens without a row or page: plan
+    again.  ``out``: buffers from batch_plan_buffers(), none of which may be an input: a loop that
     takes kv_lens of one step as cached_lens of the next keeps two sets."""
     if out is None:
         if table_capacity is None:
@@ -466,8 +467,8 @@ def janus_attn_decode_shared(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torc
                              workspace: Optional[torch.Tensor] = None):
     """Dense attention of one query token per session, q [B,H_q,d_qk] bf16, over the first prefix_len tokens, which all sessions share (pages
     prefix_table), and the session's own tokens behind them (page_tables / table_offsets of the whole sessions, as janus_batch_plan makes them).
-    kv_lens [B] int64: whole lengths, 0 for an entry that stands empty; max_len bounds them.  Pools [n_phys_pages, page_size, n_kv_heads, d] bf16 (v_pool may
-    be k_pool itself).  Returns (out [B,H_q,d_v] bf16, lse [B,H_q] fp32 | None).  `workspace` (uint8 CUDA tensor) is allocated if not given or too small."""
+    kv_lens [B] int64: whole lengths, 0 for an entry that stands empty; max_len bounds them (tightly, where the latent layout is to be fast).  Probabilities are
+    rounded to bf16, sums are fp32.  Pools [n_phys_pages, page_size, n_kv_heads, d] bf16 (v_pool may be k_pool itself).  Returns (out [B,H_q,d_v] bf16, lse [B,H_q] fp32 | None).  `workspace` (uint8 CUDA tensor) is allocated if not given or too small."""
     return _native().attn_decode_shared(q, k_pool, v_pool, prefix_table, prefix_len, page_tables, table_offsets, kv_lens, max_len, page_size, softmax_scale, d_v,
                                         want_lse, out, workspace)
 

@@ -5,8 +5,8 @@
 // session's own) and lists of tokens.  That is the way of layouts whose work is bound by the matrix units for one session already, so that reading the
 // prefix once for all gains nothing (latent: 128 heads read one row per token, 242 flops a byte), and of head dims without a kernel of their own.
 //
-// For the latent layout a session's keys are cut into pieces of equal length, each a row of the selection with an output of its own, so that every
-// pair of SMs has work whatever the sessions' lengths; the pieces that there are form a compact list, whose length the attention kernel reads from device
+// For the latent layout a session's keys are cut into pieces of equal length, each a row of the selection with an output of its own (fp32), so that every
+// pair of SMs has work; the pieces that there are form a compact list, whose length the attention kernel reads from device
 // memory, and a last kernel joins them by their log-sum-exp.
 #include "attn_shared.cuh"
 
@@ -173,8 +173,9 @@ static SlLayout sl_layout(int B, bool latent, int page_size, int64_t prefix, int
     l.width = l.prefix_pages + (max_len + page_size - 1) / page_size - prefix / page_size;
     l.k = static_cast<int>(max_len);
     if (latent) {
-        // A pair of SMs takes 1.5 us for 128 tokens and 0.6 us for a row; the rows go to 74 pairs in turn.  The length with the least time for
-        // sessions of max_len is taken (24 sessions of 9216: 1024, 216 rows).
+        // By a model in which a pair of SMs takes 1.5 us for 128 tokens (2.0 to 2.3 where all pairs are at work) and 0.6 us for a row, and the rows go to 74
+        // pairs in turn, the length with the least time for sessions of max_len (24 sessions of 9216: 1024, 216 rows).  The lengths themselves are on the device, so a
+        // loose bound costs time: 300 sessions of 1000 tokens 138 us with max_len 1024, 398 with 131072; 4 of 9000 32 and 72.
         double best = 0.;
         for (int k = 256; k <= 4096; k *= 2) {
             const int64_t rows = B * ((max_len + k - 1) / k), turns = (rows + 73) / 74;

@@ -29,7 +29,8 @@
 // the other has taken its own into registers (MMAs 900, as P . V of the other group runs between them, news of them 450, the load and news of that 660);
 // softmax 2400 beside it.  96 sessions x 32 heads in 4 groups over 65536 tokens: 116 us (890 TFLOP/s), 130 in a row of thousands, as the power limit takes the
 // clock from 1965 to some 1850 MHz.  Tiles of 80 keys, with room for two S and two P, cost the same handshakes more often: 162-174 us.  Logits handed over 64
-// keys at a time, half of S computed while the other half is read: 116 us too, as an MMA of half the keys reads all of Q again.  One warp for all MMAs: no less.
+// keys at a time, half of S computed while the other half is read: 116 us too, as an MMA of half the keys reads all of Q again.  One warp for all MMAs, with one S
+// as here: 4100 cycles a tile as well; with each group's P over an S of its own: 3865, but own tokens at 5.3 TB/s (below).
 // Fewer rows: HBM, 6.0 TB/s while tiles run (96 sessions' own tokens from 2048 to 4096: 67 us for 403 MB; P over S, an S for each group: 5.3), less with
 // small pages, as a box costs the copying some 100 cycles (8192 own tokens of 37 sessions, 8 heads of their own: pages of 64 226 us, of 16 314, of 8 445).
 // A fragment costs two to three us besides: the softmax of its last tile, P . V and the join are 1400 + 1000 + 2900 cycles.  One session of 3000 tokens: 14 us,
@@ -401,8 +402,8 @@ __global__ void __launch_bounds__(ST_THREADS, 1) attn_shared_kernel(const __grid
             if (!wait_warp(&sh->full[n % SLOTS], (n / SLOTS) & 1u)) break;
     } else if (warp == ST_QK_WARP) {
         // ================================================================== MMA issue: logits
-        // Two warps issue MMAs, one Q . K and one P . V: a wait costs a warp some 270 cycles, ready or not, and one warp for both was the bound (3500
-        // cycles for a tile of 256 rows).  What they need of one another goes by barriers.
+        // Two warps issue MMAs, one Q . K and one P . V, each in the order of its own tiles (a wait costs a warp some 270 cycles, ready or not; one warp for
+        // both took the same time a tile).  What they need of one another goes by barriers.
         constexpr uint32_t idesc = umma_idesc_major(1u, ST_ROWS, KT, 0u, 0u);
         const uint32_t q_lo = umma_desc_lo(smem_u32(q_smem), 16), k_lo = umma_desc_lo(smem_u32(ring), 16);
         uint32_t tc = 0u, n_q = 0u, n_free[2] = {0u, 0u}, light = 0u;       // phases of s_free by group; steps of fragments of 128 rows at most

@@ -188,7 +188,8 @@ __global__ void __launch_bounds__(BP_THREADS) batch_plan_kernel(const BpParams p
         if (p.key_rows != nullptr) p.key_rows[r] = key_row;
     }
     // Where the threads would go round several times, four consecutive entries at a time: one search, and their loads go together (1024 sessions
-    // of up to 131072 tokens 11.9 -> 9.2 us; eight 10.2; twelve sessions 4.7, with four entries a thread 5.4).
+    // of up to 131072 tokens, one run: one at a time 11.9 us, four 9.2, eight 10.2; the four took 10.3 to 11.0 in later runs.  Twelve sessions 4.7, with four
+    // entries a thread 5.4).
     constexpr int AT_ONCE = 4;
     const int64_t entries = page_sum[p.B];
     const int per_turn = entries > stride ? AT_ONCE : 1;
